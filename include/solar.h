@@ -301,6 +301,125 @@ solar_status solar_svd_factorize_rsvd(const void* X, const int32_t* lengths, int
                                       void* workspace, size_t workspace_bytes, void* stream);
 
 /*
+ * ---- Sequence operators ----------------------------------------------------------------------
+ * A mixing layer over a user's sequence in its order, with H heads of D columns: rotary positions, linear attention with
+ * a decay (the ordered form of solar_linear_attention, with a state that a server keeps between rows), layer norm of its
+ * heads; each with its gradient.  What differs from the conventions above: Q, K, V and their like are tensors of heads
+ * [B,N,heads,D], may lie in memory with strides, and outputs that take their place in the next operator have the inputs'
+ * type t (bf16 rounded to nearest even).  H is a multiple of Hkv; head h reads head h / (H / Hkv) of K and V.
+ *
+ * Elements between neighbouring users, rows and heads of a tensor of heads; its D columns are contiguous.  [B,N,heads,D]
+ * in order, [B,heads,N,D], and slices of a packed projection are all described so.  A stride is not negative and a
+ * multiple of 16 bytes (that of a dimension of size one is ignored); where the tensor is written no two elements share an
+ * address.
+ */
+typedef struct { int64_t batch, row, head; } solar_strides;
+
+typedef enum {
+    SOLAR_ROTARY_HALF = 0,          /* pairs (i, i + rot/2) */
+    SOLAR_ROTARY_INTERLEAVED = 1    /* pairs (2i, 2i + 1) */
+} solar_rotary_layout;
+
+typedef enum {
+    SOLAR_ROTARY_UNSCALED = 0,      /* f_i = base^(-2i/rot) */
+    SOLAR_ROTARY_LINEAR = 1,        /* f_i / factor: positions compressed by `factor` */
+    SOLAR_ROTARY_BASE = 2,          /* base * factor^(rot/(rot-2)): the slowest frequency slows by `factor`, the fastest stays */
+    SOLAR_ROTARY_BY_PARTS = 3       /* with n_i = original_length f_i / 2 pi turns over the trained length: f_i where n_i >=
+                                       turns_high, f_i / factor where n_i <= turns_low, linear in n_i between */
+} solar_rotary_scaling;
+
+/*
+ * Frequencies for solar_rotary, in HOST memory (freq [rot/2]): the caller copies them to the device once.  Arguments that
+ * a scaling does not name are ignored by it.
+ */
+solar_status solar_rotary_frequencies(int rot, double base, solar_rotary_scaling scaling, double factor,
+                                      int original_length, double turns_low, double turns_high, double* freq);
+
+/*
+ * Rotary positions for queries and keys in one launch: the pair (a, b) number i of the first `rot` columns of a head at
+ * position p becomes amplitude * (a cos x - b sin x, a sin x + b cos x) with x = p freq[i]; columns from rot on are copied.
+ *   Q  in [B,N,H,D]   K  in [B,N,Hkv,D] or NULL (then Kout is NULL too)     of type t
+ *   positions  in [B,N] int32 or NULL (row n has position n); negative ones turn backwards
+ *   freq       in [rot/2] double, DEVICE memory, 8-byte aligned; angles are formed in double precision
+ *   inverse    nonzero: -x instead of x.  With the same amplitude this is the gradient: dQ from dQout
+ *   strides    in HOST memory [4]: Q, K, Qout, Kout; NULL: all contiguous
+ *   Qout, Kout  out; each may be its input, with the same strides.  Rows at or past the valid length come out zero
+ * Supported: D a multiple of 8 up to 512, rot even, 2 <= rot <= D, B * N < 2^24.
+ */
+solar_status solar_rotary(const void* Q, const void* K, const int32_t* lengths, const int32_t* positions,
+                          const double* freq, int B, int N, int H, int Hkv, int D, int rot, solar_rotary_layout layout,
+                          int inverse, float amplitude, solar_dtype t, const solar_strides* strides, void* Qout,
+                          void* Kout, void* stream);
+
+/*
+ * Linear attention with a decay for each head.  With g_h = exp(log_decay[h]) and a state S [D,D] per user and head:
+ *   S_t = g_h S_{t-1} + k_t v_t^T,   o_t = scale S_t^T q_t = scale * sum over s <= t of g_h^(t-s) (q_t . k_s) v_s + ...
+ * the last term being scale * g_h^(t+1) S_{-1}^T q_t.  N = 1 is the step of a server that keeps the states: it reads and
+ * writes them once and needs no workspace.  Long sequences are cut into parts that are walked side by side.
+ *   Q  in [B,N,H,D]   K, V  in [B,N,Hkv,D]   of type t
+ *   log_decay  in [H] float, log g_h <= 0 (0: no decay; -infinity: no memory; nothing clamps values above 0)
+ *   state_in   in [B,H,D,D] float, S_{-1} as [k column][v column], or NULL: zeros
+ *   strides    in HOST memory [4]: Q, K, V, O; NULL: all contiguous
+ *   O          out [B,N,H,D] of type t, rows at or past the valid length zero; NULL: only the state is wanted (Q is ignored)
+ *   state_out  out [B,H,D,D] float, the state behind the last valid row; may be state_in; may be NULL if O is not.  A user of
+ *              length 0 keeps its state
+ * Sums and states are float.  A NaN or an infinity in a valid row changes outputs of its own row and later ones only (an
+ * infinity may come out as NaN).  O overlaps no input.
+ * Supported: D in {64, 128, 256}.  Workspace: solar_decay_workspace_bytes(B, N, H, Hkv, D, t, 0), which may be 0.
+ */
+size_t solar_decay_workspace_bytes(int B, int N, int H, int Hkv, int D, solar_dtype t, int backward);
+solar_status solar_decay_attention(const void* Q, const void* K, const void* V, const float* log_decay,
+                                   const int32_t* lengths, const float* state_in, int B, int N, int H, int Hkv, int D,
+                                   float scale, solar_dtype t, const solar_strides* strides, void* O, float* state_out,
+                                   void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Gradients of solar_decay_attention.  With G_t = scale q_t do_t^T + g_h G_{t+1}, dstate_out taking the place of
+ * g_h G_{t+1} at the last valid row:
+ *   dq_t = scale S_t do_t,   dk_t = G_t v_t,   dv_t = G_t^T k_t,   dstate_in = g_h G_0,
+ *   dlog_decay_h = sum over users and rows of <g_h G_t, S_{t-1}>  (formed as sum of do_t . d o_t / d log g_h).
+ * dK and dV of a head that several read are their sums.
+ *   dO          in [B,N,H,D] of type t       dstate_out  in [B,H,D,D] float or NULL: zeros
+ *   strides     in HOST memory [7]: Q, K, V, dO, dQ, dK, dV; NULL: all contiguous
+ *   dQ, dK, dV  out, of type t, rows at or past the valid length zero
+ *   dstate_in   out [B,H,D,D] float or NULL       dlog_decay  out [H] float or NULL
+ * Outputs overlap nothing.  Workspace: solar_decay_workspace_bytes(B, N, H, Hkv, D, t, 1), 256-byte aligned.
+ */
+solar_status solar_decay_attention_backward(const void* Q, const void* K, const void* V, const void* dO,
+                                            const float* log_decay, const int32_t* lengths, const float* state_in,
+                                            const float* dstate_out, int B, int N, int H, int Hkv, int D, float scale,
+                                            solar_dtype t, const solar_strides* strides, void* dQ, void* dK, void* dV,
+                                            float* dstate_in, float* dlog_decay, void* workspace,
+                                            size_t workspace_bytes, void* stream);
+
+/*
+ * Layer norm of every group of d columns: y = (x - mean) rstd weight + bias, rstd = 1/sqrt(mean((x - mean)^2) + eps).
+ * groups = 1 is the norm of whole rows; groups = H, d = D the norm of every head of [rows, H D], which a linear attention
+ * without a normalizer is followed by.
+ *   In      in [rows, groups, d] of type t_in         weight, bias  in [groups, d] float, each may be NULL (1, 0)
+ *   Out     out [rows, groups, d] of type t_out; may be In itself if the two types are the same
+ *   mean, rstd  out [rows, groups] float, for the gradient; each may be NULL
+ * Supported: d <= 16384 (any), groups * d <= 2^28, rows * groups < 2^31.
+ */
+solar_status solar_layer_norm(const void* In, const float* weight, const float* bias, int rows, int groups, int d,
+                              float eps, solar_dtype t_in, solar_dtype t_out, void* Out, float* mean, float* rstd,
+                              void* stream);
+
+/*
+ * Gradient of solar_layer_norm: with a = dOut weight and xh = (x - mean) rstd per group,
+ *   dIn = rstd (a - mean(a) - xh mean(a xh)),   dweight = sum over rows of dOut xh,   dbias = sum over rows of dOut.
+ *   mean, rstd      in, as solar_layer_norm wrote them       dOut  in [rows, groups, d] of type t_out
+ *   dIn             out [rows, groups, d] of type t_in; may be dOut, or In, if that has the same type
+ *   dweight, dbias  out [groups, d] float, each may be NULL; the order of their sums is fixed
+ * Workspace: solar_layer_norm_workspace_bytes(rows, groups, d), 256-byte aligned, if either of the two is wanted.
+ */
+size_t solar_layer_norm_workspace_bytes(int rows, int groups, int d);
+solar_status solar_layer_norm_backward(const void* In, const float* weight, const float* mean, const float* rstd,
+                                       const void* dOut, int rows, int groups, int d, solar_dtype t_in,
+                                       solar_dtype t_out, void* dIn, float* dweight, float* dbias, void* workspace,
+                                       size_t workspace_bytes, void* stream);
+
+/*
  * Per-phase timing of solar_svd_factorize, for benchmarks.  After
  * solar_phase_timing_begin() every factorize call records HIP
  * events on its stream around its three phases: the Gram contraction, the

@@ -25,6 +25,12 @@ SOLAR_BF16 = 1
 SOLAR_ATTN_SEQ_SOFTMAX = 0
 SOLAR_ATTN_EIGEN_SOFTMAX = 1
 SOLAR_ATTN_LINEAR = 2
+SOLAR_ROTARY_HALF = 0
+SOLAR_ROTARY_INTERLEAVED = 1
+SOLAR_ROTARY_UNSCALED = 0
+SOLAR_ROTARY_LINEAR = 1
+SOLAR_ROTARY_BASE = 2
+SOLAR_ROTARY_BY_PARTS = 3
 
 if not os.path.exists(LIB_PATH):
     raise ImportError(
@@ -64,6 +70,25 @@ _lib.solar_apply_weights.argtypes = [_vp, _vp, _ci, _ci, _ci, _ci, _vp, _vp]
 _lib.solar_apply_weights.restype = _ci
 _lib.solar_svd_backward.argtypes = [_vp, _vp, _vp, _vp, _vp, _ci, _ci, _ci, _ci, _cf, _vp, _vp, _sz, _vp]
 _lib.solar_svd_backward.restype = _ci
+_cd, _i64 = ctypes.c_double, ctypes.c_int64
+_lib.solar_rotary_frequencies.argtypes = [_ci, _cd, _ci, _cd, _ci, _cd, _cd, _vp]
+_lib.solar_rotary_frequencies.restype = _ci
+_lib.solar_rotary.argtypes = [_vp, _vp, _vp, _vp, _vp, _ci, _ci, _ci, _ci, _ci, _ci, _ci, _ci, _cf, _ci, _vp, _vp, _vp, _vp]
+_lib.solar_rotary.restype = _ci
+_lib.solar_decay_workspace_bytes.argtypes = [_ci, _ci, _ci, _ci, _ci, _ci, _ci]
+_lib.solar_decay_workspace_bytes.restype = _sz
+_lib.solar_decay_attention.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp, _ci, _ci, _ci, _ci, _ci, _cf, _ci, _vp, _vp, _vp, _vp,
+                                       _sz, _vp]
+_lib.solar_decay_attention.restype = _ci
+_lib.solar_decay_attention_backward.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _ci, _ci, _ci, _ci, _ci, _cf, _ci,
+                                                _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]
+_lib.solar_decay_attention_backward.restype = _ci
+_lib.solar_layer_norm.argtypes = [_vp, _vp, _vp, _ci, _ci, _ci, _cf, _ci, _ci, _vp, _vp, _vp, _vp]
+_lib.solar_layer_norm.restype = _ci
+_lib.solar_layer_norm_workspace_bytes.argtypes = [_ci, _ci, _ci]
+_lib.solar_layer_norm_workspace_bytes.restype = _sz
+_lib.solar_layer_norm_backward.argtypes = [_vp, _vp, _vp, _vp, _vp, _ci, _ci, _ci, _ci, _ci, _vp, _vp, _vp, _vp, _sz, _vp]
+_lib.solar_layer_norm_backward.restype = _ci
 _lib.solar_info_status.argtypes = [_vp, _ci]
 _lib.solar_info_status.restype = _ci
 _lib.solar_debug_option.argtypes = [_ci, _ci]
@@ -254,6 +279,196 @@ def solar_apply_weights(In, W, Out, raise_on_error: bool = True) -> int:
     if rc != SOLAR_OK and raise_on_error:
         raise SolarError(rc)
     return rc
+
+
+# ---------------------------------------------------------------------------------------
+# Sequence operators.  Tensors of heads [B,N,heads,D] may be views with any strides that include/solar.h allows (a slice of
+# a packed projection, [B,heads,N,D] transposed); the calls go to the tensors' device and its current stream.
+
+def _run(fn, tensors, args, raise_on_error: bool) -> int:
+    """fn(*args, stream) on the device that all tensors are on."""
+    dev = None
+    for t in tensors:
+        if t is None:
+            continue
+        if not t.is_cuda:
+            raise ValueError("tensors must be CUDA tensors")
+        if dev is None:
+            dev = t.device
+        elif t.device != dev:
+            raise ValueError("tensors must be on one device")
+    if dev.index == torch.cuda.current_device():
+        rc = fn(*args, torch.cuda.current_stream().cuda_stream)
+    else:
+        with torch.cuda.device(dev):
+            rc = fn(*args, torch.cuda.current_stream().cuda_stream)
+    if rc != SOLAR_OK and raise_on_error:
+        raise SolarError(rc)
+    return rc
+
+
+def _like(name: str, t: Optional[torch.Tensor], dtype, shape):
+    """data_ptr of a contiguous tensor of this type and shape, None for None."""
+    if t is None:
+        return None
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)}, got {t.dtype} "
+                         f"{tuple(t.shape)}")
+    return t.data_ptr()
+
+
+def _heads(name: str, t: torch.Tensor, dtype, shape):
+    """The three strides of a tensor of heads of this type and shape."""
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must be a {dtype} tensor of shape {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
+    st = t.stride()
+    if st[3] != 1 and shape[3] > 1:
+        raise ValueError(f"the columns of {name} must be contiguous")
+    return st[:3]
+
+
+def _strides(*strides):
+    flat = [x for s in strides for x in s]
+    return (_i64 * len(flat))(*flat)
+
+
+def _scratch(workspace: Optional[torch.Tensor]):
+    if workspace is None:
+        return None, 0
+    if not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous")
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
+def solar_rotary_frequencies(rot: int, base: float = 10000.0, scaling: int = SOLAR_ROTARY_UNSCALED, factor: float = 1.0,
+                             original_length: int = 0, turns_low: float = 1.0, turns_high: float = 32.0) -> torch.Tensor:
+    """[rot/2] double on the host; copy it to the device once."""
+    freq = torch.empty(max(int(rot) // 2, 1), dtype=torch.float64)
+    rc = _lib.solar_rotary_frequencies(int(rot), float(base), int(scaling), float(factor), int(original_length),
+                                       float(turns_low), float(turns_high), freq.data_ptr())
+    if rc != SOLAR_OK:
+        raise SolarError(rc)
+    return freq
+
+
+def solar_rotary(Q, K, freq, Qout, Kout, positions=None, lengths=None, layout: int = SOLAR_ROTARY_HALF,
+                 inverse: bool = False, amplitude: float = 1.0, raise_on_error: bool = True) -> int:
+    """Rotates the first 2 * len(freq) columns of every head of Q [B,N,H,D] and K [B,N,Hkv,D] (K and Kout may be None)."""
+    code = _dtype_code(Q)
+    B, N, H, D = Q.shape
+    sq, sqo = _heads("Q", Q, Q.dtype, Q.shape), _heads("Qout", Qout, Q.dtype, Q.shape)
+    if (K is None) != (Kout is None):
+        raise ValueError("K and Kout go together")
+    Hkv, sk, sko = 0, sq, sqo
+    if K is not None:
+        Hkv = K.shape[2]
+        sk, sko = _heads("K", K, Q.dtype, (B, N, Hkv, D)), _heads("Kout", Kout, Q.dtype, (B, N, Hkv, D))
+    args = (Q.data_ptr(), None if K is None else K.data_ptr(), _like("lengths", lengths, torch.int32, (B,)),
+            _like("positions", positions, torch.int32, (B, N)), _like("freq", freq, torch.float64, (freq.numel(),)), B, N, H,
+            Hkv, D, 2 * freq.numel(), int(layout), int(inverse), float(amplitude), code, _strides(sq, sk, sqo, sko),
+            Qout.data_ptr(), None if Kout is None else Kout.data_ptr())
+    return _run(_lib.solar_rotary, (Q, K, freq, Qout, Kout, positions, lengths), args, raise_on_error)
+
+
+def solar_decay_workspace_bytes(B: int, N: int, H: int, Hkv: int, D: int, dtype_code: int, backward: bool) -> int:
+    return int(_lib.solar_decay_workspace_bytes(B, N, H, Hkv, D, dtype_code, int(backward)))
+
+
+def solar_decay_attention(Q, K, V, log_decay, lengths, scale: float, O, state_in, state_out, workspace=None,
+                          raise_on_error: bool = True) -> int:
+    """O and state_out from Q [B,N,H,D], K and V [B,N,Hkv,D]; Q and O may be None (the state alone)."""
+    code = _dtype_code(K)
+    B, N, Hkv, D = K.shape
+    H = log_decay.numel()
+    sk, sv = _heads("K", K, K.dtype, K.shape), _heads("V", V, K.dtype, K.shape)
+    sq = so = (0, 0, 0)
+    if O is not None:
+        sq, so = _heads("Q", Q, K.dtype, (B, N, H, D)), _heads("O", O, K.dtype, (B, N, H, D))
+    ws, wsb = _scratch(workspace)
+    args = (None if O is None else Q.data_ptr(), K.data_ptr(), V.data_ptr(),
+            _like("log_decay", log_decay, torch.float32, (H,)), _like("lengths", lengths, torch.int32, (B,)),
+            _like("state_in", state_in, torch.float32, (B, H, D, D)), B, N, H, Hkv, D, float(scale), code,
+            _strides(sq, sk, sv, so), None if O is None else O.data_ptr(),
+            _like("state_out", state_out, torch.float32, (B, H, D, D)), ws, wsb)
+    return _run(_lib.solar_decay_attention,
+                (Q if O is not None else None, K, V, log_decay, lengths, O, state_in, state_out, workspace), args,
+                raise_on_error)
+
+
+def solar_decay_attention_backward(Q, K, V, dO, log_decay, lengths, scale: float, state_in, dstate_out, dQ, dK, dV,
+                                   dstate_in, dlog_decay, workspace, raise_on_error: bool = True) -> int:
+    """Gradients of solar_decay_attention; state_in, dstate_out, dstate_in and dlog_decay may be None."""
+    code = _dtype_code(Q)
+    B, N, H, D = Q.shape
+    Hkv = K.shape[2]
+    shape, shared, dt = (B, N, H, D), (B, N, Hkv, D), Q.dtype
+    st = _strides(_heads("Q", Q, dt, shape), _heads("K", K, dt, shared), _heads("V", V, dt, shared),
+                  _heads("dO", dO, dt, shape), _heads("dQ", dQ, dt, shape), _heads("dK", dK, dt, shared),
+                  _heads("dV", dV, dt, shared))
+    ws, wsb = _scratch(workspace)
+    states = (B, H, D, D)
+    args = (Q.data_ptr(), K.data_ptr(), V.data_ptr(), dO.data_ptr(), _like("log_decay", log_decay, torch.float32, (H,)),
+            _like("lengths", lengths, torch.int32, (B,)), _like("state_in", state_in, torch.float32, states),
+            _like("dstate_out", dstate_out, torch.float32, states), B, N, H, Hkv, D, float(scale), code, st, dQ.data_ptr(),
+            dK.data_ptr(), dV.data_ptr(), _like("dstate_in", dstate_in, torch.float32, states),
+            _like("dlog_decay", dlog_decay, torch.float32, (H,)), ws, wsb)
+    return _run(_lib.solar_decay_attention_backward,
+                (Q, K, V, dO, log_decay, lengths, state_in, dstate_out, dQ, dK, dV, dstate_in, dlog_decay, workspace), args,
+                raise_on_error)
+
+
+def _norm_sizes(In, weight, bias):
+    """(rows, groups, d): the weight [d] or [groups, d] says what is normalised, or the last dimension without one."""
+    p = weight if weight is not None else bias
+    if p is None:
+        groups, d = 1, In.shape[-1]
+    else:
+        groups, d = (1, p.shape[0]) if p.dim() == 1 else (p.shape[0], p.shape[1])
+    if In.dim() == 0 or groups * d == 0 or In.numel() % (groups * d) or (In.shape[-1] not in (d, groups * d)) or (
+            groups > 1 and In.shape[-1] == d and (In.dim() < 2 or In.shape[-2] != groups)):
+        raise ValueError(f"a weight of {groups} x {d} does not fit an input of shape {tuple(In.shape)}")
+    return In.numel() // (groups * d), groups, d
+
+
+def _param(name: str, t, groups: int, d: int):
+    return None if t is None else _like(name, t, torch.float32, (d,) if t.dim() == 1 and groups == 1 else (groups, d))
+
+
+def solar_layer_norm(In, weight, bias, eps: float, Out, mean=None, rstd=None, raise_on_error: bool = True) -> int:
+    """Layer norm of In [..., groups, d], [..., groups * d] or [..., d] with weight and bias [groups, d] or [d]."""
+    _check(In, Out, mean, rstd)
+    rows, groups, d = _norm_sizes(In, weight, bias)
+    if Out.shape != In.shape:
+        raise ValueError("Out must have the shape of In")
+    for name, t in (("mean", mean), ("rstd", rstd)):
+        if t is not None and (t.dtype != torch.float32 or t.numel() != rows * groups):
+            raise ValueError(f"{name} must hold {rows * groups} float32 values")
+    args = (In.data_ptr(), _param("weight", weight, groups, d), _param("bias", bias, groups, d), rows, groups, d, float(eps),
+            _dtype_code(In), _dtype_code(Out), Out.data_ptr(), None if mean is None else mean.data_ptr(),
+            None if rstd is None else rstd.data_ptr())
+    return _run(_lib.solar_layer_norm, (In, weight, bias, Out, mean, rstd), args, raise_on_error)
+
+
+def solar_layer_norm_workspace_bytes(rows: int, groups: int, d: int) -> int:
+    return int(_lib.solar_layer_norm_workspace_bytes(rows, groups, d))
+
+
+def solar_layer_norm_backward(In, weight, mean, rstd, dOut, dIn, dweight, dbias, workspace=None,
+                              raise_on_error: bool = True) -> int:
+    """Gradients of solar_layer_norm; dweight and dbias may be None."""
+    _check(In, mean, rstd, dOut, dIn, dweight, dbias, workspace)
+    rows, groups, d = _norm_sizes(In, weight if weight is not None else dweight, dbias)
+    if dOut.shape != In.shape or dIn.shape != In.shape or dIn.dtype != In.dtype:
+        raise ValueError("dOut and dIn must have the shape of In, and dIn its type")
+    for name, t in (("mean", mean), ("rstd", rstd)):
+        if t.dtype != torch.float32 or t.numel() != rows * groups:
+            raise ValueError(f"{name} must hold {rows * groups} float32 values")
+    ws, wsb = _scratch(workspace)
+    args = (In.data_ptr(), _param("weight", weight, groups, d), mean.data_ptr(), rstd.data_ptr(), dOut.data_ptr(), rows,
+            groups, d, _dtype_code(In), _dtype_code(dOut), dIn.data_ptr(), _param("dweight", dweight, groups, d),
+            _param("dbias", dbias, groups, d), ws, wsb)
+    return _run(_lib.solar_layer_norm_backward, (In, weight, mean, rstd, dOut, dIn, dweight, dbias, workspace), args,
+                raise_on_error)
 
 
 # ---------------------------------------------------------------------------------------

@@ -1,0 +1,186 @@
+// Linear attention with a decay for each head, row by row: S_t = g S_{t-1} + k_t v_t^T, o_t = S_t^T q_t.
+//
+// The state is cut into slices of 32 columns, one workgroup each: eight lanes hold four columns, 32 groups of lanes hold
+// D / 32 rows each, in registers from the first row of the sequence to the last.  A row costs one sum over the groups
+// (three steps across lanes, one through LDS).
+#include "sequence.h"
+
+namespace solar {
+
+namespace {
+
+constexpr int kSlice = 32;      // columns of the state per workgroup
+constexpr int kThreads = 256;
+
+template <bool BF16>
+__device__ __forceinline__ float load1(const char* p, int i) {
+    if constexpr (BF16) return __uint_as_float((uint32_t)reinterpret_cast<const uint16_t*>(p)[i] << 16);
+    else return reinterpret_cast<const float*>(p)[i];
+}
+
+template <int D, bool BF16, bool REVERSE, bool MOMENT>
+__global__ __launch_bounds__(kThreads) void decay_rows_kernel(Walk w) {
+    constexpr int RPT = D / 32;             // rows of the state per thread
+    constexpr int NS = D / kSlice;
+    __shared__ float part[2][4][kSlice];
+    const int slice = blockIdx.x % NS, h = blockIdx.x / NS % w.H, b = blockIdx.x / NS / w.H;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int row0 = (tid >> 3) * RPT, col = slice * kSlice + 4 * (tid & 7);
+    // g - 1, and g x as x + (g - 1) x: over thousands of rows the error of a rounded g would add up, near g = 1 in particular
+    const float g1 = expm1f(w.log_decay[h]);
+    const size_t at = ((size_t)b * w.H + h) * D * D;
+    const int len = user_len(w.lengths, b, w.N);
+    float S[RPT][4], T[MOMENT ? RPT : 1][4];
+#pragma unroll
+    for (int i = 0; i < RPT; ++i)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            S[i][c] = 0.f;
+            if (w.state_in)
+                S[i][c] = w.in_turned ? w.state_in[at + (size_t)(col + c) * D + row0 + i]
+                                      : w.state_in[at + (size_t)(row0 + i) * D + col + c];
+            if constexpr (MOMENT) T[i][c] = 0.f;
+        }
+    float z = 0.f;
+    for (int i = 0; i < len; ++i) {
+        const int t = REVERSE ? len - 1 - i : i;
+        const char *q = row_of(w.q, b, t, h), *k = row_of(w.k, b, t, h), *v = row_of(w.v, b, t, h);
+        float o[4] = {0.f, 0.f, 0.f, 0.f};
+        float vv[4];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) vv[c] = w.kv_scale * load1<BF16>(v, col + c);
+#pragma unroll
+        for (int r = 0; r < RPT; ++r) {
+            const float kr = load1<BF16>(k, row0 + r), qr = load1<BF16>(q, row0 + r);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                if constexpr (MOMENT) {
+                    const float x = T[r][c] + S[r][c];
+                    T[r][c] = fmaf(x, g1, x);
+                }
+                if constexpr (!REVERSE) S[r][c] = fmaf(S[r][c], g1, S[r][c]);
+                S[r][c] = fmaf(kr, vv[c], S[r][c]);
+                o[c] = fmaf(qr, MOMENT ? T[r][c] : S[r][c], o[c]);
+                if constexpr (REVERSE) S[r][c] = fmaf(S[r][c], g1, S[r][c]);
+            }
+        }
+        if (!w.o.data && !MOMENT) continue;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            o[c] += __shfl_xor(o[c], 8);
+            o[c] += __shfl_xor(o[c], 16);
+            o[c] += __shfl_xor(o[c], 32);
+            if (lane < 8) part[i & 1][wave][4 * lane + c] = o[c];
+        }
+        __syncthreads();        // the other half of `part` is free again: everybody has read it before coming here
+        if (tid < kSlice) {
+            float s = 0.f;
+#pragma unroll
+            for (int y = 0; y < 4; ++y) s += part[i & 1][y][tid];
+            s *= w.o_scale;
+            const int c = slice * kSlice + tid;
+            if constexpr (MOMENT) {
+                z = fmaf(s, load1<BF16>(row_of(w.grad, b, t, h), c), z);
+            } else {
+                char* out = row_of(w.o, b, t, h);
+                if (BF16 && !w.o_float) reinterpret_cast<__bf16*>(out)[c] = (__bf16)s;
+                else reinterpret_cast<float*>(out)[c] = s;
+            }
+        }
+    }
+    if constexpr (MOMENT) {
+        if (w.grad_state) {
+#pragma unroll
+            for (int r = 0; r < RPT; ++r)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) z = fmaf(w.grad_state[at + (size_t)(row0 + r) * D + col + c], T[r][c], z);
+        }
+#pragma unroll
+        for (int m = 32; m; m >>= 1) z += __shfl_xor(z, m);
+        __syncthreads();
+        if (lane == 0) part[0][wave][0] = z;
+        __syncthreads();
+        if (tid == 0) w.moments[blockIdx.x] = part[0][0][0] + part[0][1][0] + part[0][2][0] + part[0][3][0];
+        return;
+    }
+    if (w.o.data && tid < kSlice) {
+        for (int t = len; t < w.N; ++t) {
+            char* out = row_of(w.o, b, t, h);
+            const int c = slice * kSlice + tid;
+            if (BF16 && !w.o_float) reinterpret_cast<__bf16*>(out)[c] = (__bf16)0.f;
+            else reinterpret_cast<float*>(out)[c] = 0.f;
+        }
+    }
+    if (w.state_out) {
+#pragma unroll
+        for (int r = 0; r < RPT; ++r)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) w.state_out[at + (size_t)(row0 + r) * D + col + c] = S[r][c];
+    }
+}
+
+template <int D, bool BF16>
+void launch_rows(const Walk& w, hipStream_t stream) {
+    const dim3 grid(w.B * w.H * (D / kSlice)), block(kThreads);
+    if (w.moment) hipLaunchKernelGGL((decay_rows_kernel<D, BF16, false, true>), grid, block, 0, stream, w);
+    else if (w.reverse) hipLaunchKernelGGL((decay_rows_kernel<D, BF16, true, false>), grid, block, 0, stream, w);
+    else hipLaunchKernelGGL((decay_rows_kernel<D, BF16, false, false>), grid, block, 0, stream, w);
+}
+
+__global__ __launch_bounds__(64) void moment_sum_kernel(const float* __restrict__ m, int B, int H, int slices, float* dlog) {
+    const int h = blockIdx.x;
+    double s = 0.;
+    for (int i = threadIdx.x; i < B * slices; i += 64) s += m[((size_t)(i / slices) * H + h) * slices + i % slices];
+    for (int x = 32; x; x >>= 1) s += __shfl_xor(s, x);
+    if (threadIdx.x == 0) dlog[h] = (float)s;
+}
+
+// a thread takes four columns of one row and shared head
+__global__ __launch_bounds__(256) void share_sum_kernel(const float* __restrict__ in, int B, int N, int H, int Hkv, int D,
+                                                        Heads out, bool bf16) {
+    const int share = H / Hkv, vecs = D / 4;
+    const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= (size_t)B * N * Hkv * vecs) return;
+    const int c = 4 * (int)(i % vecs), hk = (int)(i / vecs % Hkv);
+    const size_t bn = i / vecs / Hkv;
+    const float* p = in + (bn * H + (size_t)hk * share) * D + c;
+    v4f s = *reinterpret_cast<const v4f*>(p);
+    for (int j = 1; j < share; ++j) s += *reinterpret_cast<const v4f*>(p + (size_t)j * D);
+    char* o = row_of(out, (int)(bn / N), (int64_t)(bn % N), hk);
+    if (bf16) {
+        typedef __bf16 v4bf __attribute__((ext_vector_type(4)));
+        v4bf r = {(__bf16)s[0], (__bf16)s[1], (__bf16)s[2], (__bf16)s[3]};
+        *reinterpret_cast<v4bf*>(o + 2 * c) = r;
+    } else {
+        *reinterpret_cast<v4f*>(o + 4 * c) = s;
+    }
+}
+
+}  // namespace
+
+int decay_slices(int D) { return D / kSlice; }
+
+hipError_t launch_decay_walk(const Walk& w, hipStream_t stream) {
+    switch (w.D) {
+        case 64: w.bf16 ? launch_rows<64, true>(w, stream) : launch_rows<64, false>(w, stream); break;
+        case 128: w.bf16 ? launch_rows<128, true>(w, stream) : launch_rows<128, false>(w, stream); break;
+        case 256: w.bf16 ? launch_rows<256, true>(w, stream) : launch_rows<256, false>(w, stream); break;
+        default: return hipErrorInvalidValue;
+    }
+    return hipGetLastError();
+}
+
+hipError_t launch_moment_sum(const float* moments, int B, int H, int slices, float* dlog, hipStream_t stream) {
+    hipLaunchKernelGGL(moment_sum_kernel, dim3(H), dim3(64), 0, stream, moments, B, H, slices, dlog);
+    return hipGetLastError();
+}
+
+hipError_t launch_share_sum(const float* in, int B, int N, int H, int Hkv, int D, const Heads& out, bool bf16,
+                            hipStream_t stream) {
+    const size_t n = (size_t)B * N * Hkv * (D / 4);
+    hipLaunchKernelGGL(share_sum_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, stream, in, B, N, H, Hkv, D,
+                       out, bf16);
+    return hipGetLastError();
+}
+
+}  // namespace solar

@@ -1,0 +1,77 @@
+// Kernels' parameters and host-side launchers of the sequence operators (internal to the library): rotary positions,
+// linear attention with a decay, layer norm.
+#pragma once
+
+#include "common.h"
+
+namespace solar {
+
+// Elements between users, rows and heads.
+struct Strides {
+    int64_t batch, row, head;
+};
+
+// One tensor of heads: head h of the operator reads (or writes) head h / share of it.
+struct Heads {
+    char* data;
+    Strides s;      // in bytes
+    int share;
+};
+
+__device__ __forceinline__ char* row_of(const Heads& t, int b, int64_t n, int h) {
+    return t.data + b * t.s.batch + n * t.s.row + (int64_t)(h / t.share) * t.s.head;
+}
+
+// One walk over the rows of every user and head with a state S [D,D]:
+//   forward   S = g S + k_t v_t^T,  o_t = o_scale S^T q_t          rows 0 .. len - 1
+//   reverse   S += k_t v_t^T,  o_t = o_scale S^T q_t,  S = g S     rows len - 1 .. 0
+// with kv_scale on every k_t v_t^T.  The gradients of the operator are walks with the tensors in other roles.
+struct Walk {
+    Heads q, k, v, o;               // o.data may be null: the last state alone
+    const int32_t* lengths;
+    const float* log_decay;         // [H]
+    const float* state_in;          // [B,H,D,D], null: zeros
+    float* state_out;               // [B,H,D,D] or null
+    int B, N, H, D;
+    float o_scale, kv_scale;
+    bool reverse, in_turned;        // in_turned: state_in is read transposed
+    bool bf16, o_float;             // o_float: o is float whatever the inputs are
+    // the derivative by log g instead of o: `grad` is the gradient of o, `grad_state` of the last state (or null)
+    bool moment;
+    Heads grad;
+    const float* grad_state;
+    float* moments;                 // [B][H][slices] partial sums
+};
+
+// decay.hip
+int decay_slices(int D);
+hipError_t launch_decay_walk(const Walk& w, hipStream_t stream);
+// dlog[h] = the sum of moments [B][H][slices] over users and slices
+hipError_t launch_moment_sum(const float* moments, int B, int H, int slices, float* dlog, hipStream_t stream);
+// out [.., Hkv, D] = the sum of in [B,N,H,D] over the H / Hkv heads that share one
+hipError_t launch_share_sum(const float* in, int B, int N, int H, int Hkv, int D, const Heads& out, bool bf16,
+                            hipStream_t stream);
+
+// rotary.hip
+struct Rotary {
+    Heads in[2], out[2];            // queries and keys; heads[1] = 0: queries alone
+    int heads[2];
+    const int32_t *lengths, *positions;
+    const double* freq;             // [rot / 2] radians per position
+    int B, N, D, rot;
+    bool interleaved, inverse, bf16;
+    float amplitude;
+};
+hipError_t launch_rotary(const Rotary& r, hipStream_t stream);
+
+// norm.hip
+constexpr int kNormMaxD = 16384;
+size_t norm_partial_floats(int rows, int groups, int d);
+hipError_t launch_layer_norm(const void* in, const float* weight, const float* bias, int rows, int groups, int d,
+                             float eps, bool in_bf16, bool out_bf16, void* out, float* mean, float* rstd,
+                             hipStream_t stream);
+hipError_t launch_layer_norm_backward(const void* in, const float* weight, const float* mean, const float* rstd,
+                                      const void* dout, int rows, int groups, int d, bool in_bf16, bool dout_bf16,
+                                      void* din, float* dweight, float* dbias, float* partials, hipStream_t stream);
+
+}  // namespace solar
