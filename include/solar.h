@@ -365,7 +365,8 @@ solar_status solar_rotary(const void* Q, const void* K, const int32_t* lengths, 
  *              length 0 keeps its state
  * Sums and states are float.  A NaN or an infinity in a valid row changes outputs of its own row and later ones only (an
  * infinity may come out as NaN).  O overlaps no input.
- * Supported: D in {64, 128, 256}.  Workspace: solar_decay_workspace_bytes(B, N, H, Hkv, D, t, 0), which may be 0.
+ * Supported: D in {64, 128, 256}, N <= 2^30, rows less than 16 MB apart.  Workspace: solar_decay_workspace_bytes(B, N, H, Hkv, D,
+ * t, 0) bytes, which may be 0, 256-byte aligned.
  */
 size_t solar_decay_workspace_bytes(int B, int N, int H, int Hkv, int D, solar_dtype t, int backward);
 solar_status solar_decay_attention(const void* Q, const void* K, const void* V, const float* log_decay,

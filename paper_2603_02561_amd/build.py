@@ -11,7 +11,7 @@ CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libsolar.so")
 SOURCES = ["api", "gram", "eig", "project", "rsvd", "rsvd_small", "attention", "attention_x32", "linear", "backward", "dense_ref",
-           "api_sequence", "decay", "rotary", "norm"]
+           "api_sequence", "decay", "decay_chunk", "rotary", "norm"]
 FLAGS = ["-O3", "--offload-arch=gfx950", "-std=c++17", "-fPIC",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 # eig.hip is bound by chains of dependent instructions on waves that have a SIMD to themselves: its

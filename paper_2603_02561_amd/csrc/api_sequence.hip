@@ -50,21 +50,30 @@ bool take(const void* p, const solar_strides* s, int B, int N, int heads, int D,
 
 bool known(solar_dtype t) { return t == SOLAR_F32 || t == SOLAR_BF16; }
 
+// The kernels of the decayed attention step through up to 64 rows with 32-bit offsets.
+bool rows_near(const Heads& t) { return t.s.row < (1 << 24); }
+
 solar_status check_decay(int B, int N, int H, int Hkv, int D, float scale, solar_dtype t) {
     if (B <= 0 || N <= 0 || H <= 0 || Hkv <= 0 || D <= 0 || !known(t) || H % Hkv || !std::isfinite(scale))
         return SOLAR_ERR_INVALID_ARG;
     if (D != 64 && D != 128 && D != 256) return SOLAR_ERR_UNSUPPORTED;
-    if ((int64_t)B * H * decay_slices(D) > kMaxBlocks) return SOLAR_ERR_UNSUPPORTED;
+    if (N > 1 << 30) return SOLAR_ERR_UNSUPPORTED;
+    // workgroups of the row form and of the chunked form, which go by users, heads and slices, and no part is cut below 512 rows
+    const int64_t slices = D / 32, parts = 1 + N / 512;
+    if ((int64_t)B * H * slices > kMaxBlocks / 2 || (int64_t)B * H * slices > kMaxBlocks / 2 * 512 / parts)
+        return SOLAR_ERR_UNSUPPORTED;
     return SOLAR_OK;
 }
 
 struct DecayCarve {
-    float *dk, *dv;     // [B,N,H,D] of every head, where heads share K and V
-    float* moments;     // [B,H,slices]
+    DecayParts cut;
+    float *parts, *part_moments;    // [B,H,parts-1,D,D]
+    float *dk, *dv;                 // [B,N,H,D] of every head, where heads share K and V
+    double* moments;                // [B,H,parts,slices]
     size_t total;
 };
 
-DecayCarve carve_decay(void* ws, int B, int N, int H, int Hkv, int D, bool backward) {
+DecayCarve carve_decay(void* ws, int B, int N, int H, int Hkv, int D, bool bf16, bool backward) {
     DecayCarve c = {};
     char* at = static_cast<char*>(ws);
     auto part = [&](size_t floats) {
@@ -72,11 +81,16 @@ DecayCarve carve_decay(void* ws, int B, int N, int H, int Hkv, int D, bool backw
         at += align256(sizeof(float) * floats);
         return p;
     };
+    if (!backward && N <= kDecayRows) return c;
+    c.cut = decay_parts(B, N, H, D, bf16);
+    const size_t states = (size_t)B * H * (c.cut.parts - 1) * D * D;
+    c.parts = part(states);
     if (backward) {
         const size_t shared = H != Hkv ? (size_t)B * N * H * D : 0;
+        c.part_moments = part(states);
         c.dk = part(shared);
         c.dv = part(shared);
-        c.moments = part((size_t)B * H * decay_slices(D));
+        c.moments = reinterpret_cast<double*>(part((size_t)2 * B * H * c.cut.parts * moment_slices(D)));
     }
     c.total = (size_t)(at - static_cast<char*>(ws));
     return c;
@@ -148,7 +162,7 @@ solar_status solar_rotary(const void* Q, const void* K, const int32_t* lengths, 
 
 size_t solar_decay_workspace_bytes(int B, int N, int H, int Hkv, int D, solar_dtype t, int backward) {
     if (check_decay(B, N, H, Hkv, D, 1.f, t) != SOLAR_OK) return 0;
-    return carve_decay(nullptr, B, N, H, Hkv, D, backward != 0).total;
+    return carve_decay(nullptr, B, N, H, Hkv, D, t == SOLAR_BF16, backward != 0).total;
 }
 
 solar_status solar_decay_attention(const void* Q, const void* K, const void* V, const float* log_decay,
@@ -172,7 +186,8 @@ solar_status solar_decay_attention(const void* Q, const void* K, const void* V, 
     } else {
         w.q = w.k;
     }
-    const DecayCarve c = carve_decay(workspace, B, N, H, Hkv, D, false);
+    if (!rows_near(w.k) || !rows_near(w.v) || !rows_near(w.q) || !rows_near(w.o)) return SOLAR_ERR_UNSUPPORTED;
+    const DecayCarve c = carve_decay(workspace, B, N, H, Hkv, D, t == SOLAR_BF16, false);
     if (c.total && (!workspace || workspace_bytes < c.total || misaligned(workspace, 256))) return SOLAR_ERR_WORKSPACE;
     w.lengths = lengths;
     w.log_decay = log_decay;
@@ -182,7 +197,12 @@ solar_status solar_decay_attention(const void* Q, const void* K, const void* V, 
     w.o_scale = scale;
     w.kv_scale = 1.f;
     w.bf16 = t == SOLAR_BF16;
-    return launch_decay_walk(w, (hipStream_t)stream) == hipSuccess ? SOLAR_OK : SOLAR_ERR_HIP;
+    w.nparts = c.cut.parts;
+    w.part_rows = c.cut.rows;
+    w.parts = c.parts;
+    const hipError_t e = N <= kDecayRows ? launch_decay_rows(w, (hipStream_t)stream)
+                                         : launch_decay_chunks(w, (hipStream_t)stream);
+    return e == hipSuccess ? SOLAR_OK : SOLAR_ERR_HIP;
 }
 
 solar_status solar_decay_attention_backward(const void* Q, const void* K, const void* V, const void* dO,
@@ -204,7 +224,10 @@ solar_status solar_decay_attention_backward(const void* Q, const void* K, const 
         !take(dQ, at(4), B, N, H, D, es, 1, true, &dq) || !take(dK, at(5), B, N, Hkv, D, es, 1, true, &dk) ||
         !take(dV, at(6), B, N, Hkv, D, es, 1, true, &dv))
         return SOLAR_ERR_INVALID_ARG;
-    const DecayCarve c = carve_decay(workspace, B, N, H, Hkv, D, true);
+    for (const Heads& x : {q, k, vv, g, dq, dk, dv})
+        if (!rows_near(x)) return SOLAR_ERR_UNSUPPORTED;
+    if ((int64_t)H * D > 1 << 22) return SOLAR_ERR_UNSUPPORTED;      // rows of the float work arrays
+    const DecayCarve c = carve_decay(workspace, B, N, H, Hkv, D, t == SOLAR_BF16, true);
     if (c.total && (!workspace || workspace_bytes < c.total || misaligned(workspace, 256))) return SOLAR_ERR_WORKSPACE;
     if ((int64_t)B * N * Hkv * (D / 4) > kMaxBlocks * 256) return SOLAR_ERR_UNSUPPORTED;
     hipStream_t st = (hipStream_t)stream;
@@ -213,6 +236,10 @@ solar_status solar_decay_attention_backward(const void* Q, const void* K, const 
     w.log_decay = log_decay;
     w.B = B; w.N = N; w.H = H; w.D = D;
     w.bf16 = t == SOLAR_BF16;
+    w.nparts = c.cut.parts;
+    w.part_rows = c.cut.rows;
+    w.parts = c.parts;
+    w.part_moments = c.part_moments;
     // dq_t = scale S_t do_t: the same walk with do for q, v for k and k for v, its state transposed
     Walk a = w;
     a.q = g; a.k = vv; a.v = k; a.o = dq;
@@ -220,7 +247,7 @@ solar_status solar_decay_attention_backward(const void* Q, const void* K, const 
     a.in_turned = true;
     a.o_scale = scale;
     a.kv_scale = 1.f;
-    hipError_t e = launch_decay_walk(a, st);
+    hipError_t e = launch_decay_chunks(a, st);
     if (e != hipSuccess) return SOLAR_ERR_HIP;
     // dv_t = G_t^T k_t, dk_t = G_t v_t with G_t = scale q_t do_t^T + g G_{t+1}: walks from the last row on
     Walk d = w;
@@ -233,13 +260,13 @@ solar_status solar_decay_attention_backward(const void* Q, const void* K, const 
     if (share > 1 && !take(c.dv, nullptr, B, N, H, D, sizeof(float), 1, true, &part)) return SOLAR_ERR_WORKSPACE;
     d.q = k; d.k = q; d.v = g; d.o = share > 1 ? part : dv;
     d.state_out = dstate_in;
-    e = launch_decay_walk(d, st);
+    e = launch_decay_chunks(d, st);
     if (e != hipSuccess) return SOLAR_ERR_HIP;
     if (share > 1) part.data = reinterpret_cast<char*>(c.dk);
     d.q = vv; d.k = g; d.v = q; d.o = share > 1 ? part : dk;
     d.in_turned = true;
     d.state_out = nullptr;
-    e = launch_decay_walk(d, st);
+    e = launch_decay_chunks(d, st);
     if (e != hipSuccess) return SOLAR_ERR_HIP;
     if (share > 1) {
         e = launch_share_sum(c.dk, B, N, H, Hkv, D, dk, w.bf16, st);
@@ -258,9 +285,9 @@ solar_status solar_decay_attention_backward(const void* Q, const void* K, const 
         m.grad = g;
         m.grad_state = dstate_out;
         m.moments = c.moments;
-        e = launch_decay_walk(m, st);
+        e = launch_decay_chunks(m, st);
         if (e != hipSuccess) return SOLAR_ERR_HIP;
-        e = launch_moment_sum(c.moments, B, H, decay_slices(D), dlog_decay, st);
+        e = launch_moment_sum(c.moments, B, H, c.cut.parts * moment_slices(D), dlog_decay, st);
         if (e != hipSuccess) return SOLAR_ERR_HIP;
     }
     return SOLAR_OK;

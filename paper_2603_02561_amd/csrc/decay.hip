@@ -1,4 +1,5 @@
-// Linear attention with a decay for each head, row by row: S_t = g S_{t-1} + k_t v_t^T, o_t = S_t^T q_t.
+// Linear attention with a decay for each head, row by row: S_t = g S_{t-1} + k_t v_t^T, o_t = scale S_t^T q_t; the form for
+// single tokens, bound by reading and writing the states.
 //
 // The state is cut into slices of 32 columns, one workgroup each: eight lanes hold four columns, 32 groups of lanes hold
 // D / 32 rows each, in registers from the first row of the sequence to the last.  A row costs one sum over the groups
@@ -18,7 +19,7 @@ __device__ __forceinline__ float load1(const char* p, int i) {
     else return reinterpret_cast<const float*>(p)[i];
 }
 
-template <int D, bool BF16, bool REVERSE, bool MOMENT>
+template <int D, bool BF16>
 __global__ __launch_bounds__(kThreads) void decay_rows_kernel(Walk w) {
     constexpr int RPT = D / 32;             // rows of the state per thread
     constexpr int NS = D / kSlice;
@@ -30,84 +31,54 @@ __global__ __launch_bounds__(kThreads) void decay_rows_kernel(Walk w) {
     const float g1 = expm1f(w.log_decay[h]);
     const size_t at = ((size_t)b * w.H + h) * D * D;
     const int len = user_len(w.lengths, b, w.N);
-    float S[RPT][4], T[MOMENT ? RPT : 1][4];
+    float S[RPT][4];
 #pragma unroll
     for (int i = 0; i < RPT; ++i)
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
             S[i][c] = 0.f;
-            if (w.state_in)
-                S[i][c] = w.in_turned ? w.state_in[at + (size_t)(col + c) * D + row0 + i]
-                                      : w.state_in[at + (size_t)(row0 + i) * D + col + c];
-            if constexpr (MOMENT) T[i][c] = 0.f;
+            if (w.state_in) S[i][c] = w.state_in[at + (size_t)(row0 + i) * D + col + c];
         }
-    float z = 0.f;
-    for (int i = 0; i < len; ++i) {
-        const int t = REVERSE ? len - 1 - i : i;
+    for (int t = 0; t < len; ++t) {
         const char *q = row_of(w.q, b, t, h), *k = row_of(w.k, b, t, h), *v = row_of(w.v, b, t, h);
         float o[4] = {0.f, 0.f, 0.f, 0.f};
         float vv[4];
 #pragma unroll
-        for (int c = 0; c < 4; ++c) vv[c] = w.kv_scale * load1<BF16>(v, col + c);
+        for (int c = 0; c < 4; ++c) vv[c] = load1<BF16>(v, col + c);
 #pragma unroll
         for (int r = 0; r < RPT; ++r) {
             const float kr = load1<BF16>(k, row0 + r), qr = load1<BF16>(q, row0 + r);
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
-                if constexpr (MOMENT) {
-                    const float x = T[r][c] + S[r][c];
-                    T[r][c] = fmaf(x, g1, x);
-                }
-                if constexpr (!REVERSE) S[r][c] = fmaf(S[r][c], g1, S[r][c]);
-                S[r][c] = fmaf(kr, vv[c], S[r][c]);
-                o[c] = fmaf(qr, MOMENT ? T[r][c] : S[r][c], o[c]);
-                if constexpr (REVERSE) S[r][c] = fmaf(S[r][c], g1, S[r][c]);
+                S[r][c] = fmaf(kr, vv[c], fmaf(S[r][c], g1, S[r][c]));
+                o[c] = fmaf(qr, S[r][c], o[c]);
             }
         }
-        if (!w.o.data && !MOMENT) continue;
+        if (!w.o.data) continue;
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
             o[c] += __shfl_xor(o[c], 8);
             o[c] += __shfl_xor(o[c], 16);
             o[c] += __shfl_xor(o[c], 32);
-            if (lane < 8) part[i & 1][wave][4 * lane + c] = o[c];
+            if (lane < 8) part[t & 1][wave][4 * lane + c] = o[c];
         }
         __syncthreads();        // the other half of `part` is free again: everybody has read it before coming here
         if (tid < kSlice) {
             float s = 0.f;
 #pragma unroll
-            for (int y = 0; y < 4; ++y) s += part[i & 1][y][tid];
+            for (int y = 0; y < 4; ++y) s += part[t & 1][y][tid];
             s *= w.o_scale;
             const int c = slice * kSlice + tid;
-            if constexpr (MOMENT) {
-                z = fmaf(s, load1<BF16>(row_of(w.grad, b, t, h), c), z);
-            } else {
-                char* out = row_of(w.o, b, t, h);
-                if (BF16 && !w.o_float) reinterpret_cast<__bf16*>(out)[c] = (__bf16)s;
-                else reinterpret_cast<float*>(out)[c] = s;
-            }
+            char* out = row_of(w.o, b, t, h);
+            if constexpr (BF16) reinterpret_cast<__bf16*>(out)[c] = (__bf16)s;
+            else reinterpret_cast<float*>(out)[c] = s;
         }
-    }
-    if constexpr (MOMENT) {
-        if (w.grad_state) {
-#pragma unroll
-            for (int r = 0; r < RPT; ++r)
-#pragma unroll
-                for (int c = 0; c < 4; ++c) z = fmaf(w.grad_state[at + (size_t)(row0 + r) * D + col + c], T[r][c], z);
-        }
-#pragma unroll
-        for (int m = 32; m; m >>= 1) z += __shfl_xor(z, m);
-        __syncthreads();
-        if (lane == 0) part[0][wave][0] = z;
-        __syncthreads();
-        if (tid == 0) w.moments[blockIdx.x] = part[0][0][0] + part[0][1][0] + part[0][2][0] + part[0][3][0];
-        return;
     }
     if (w.o.data && tid < kSlice) {
         for (int t = len; t < w.N; ++t) {
             char* out = row_of(w.o, b, t, h);
             const int c = slice * kSlice + tid;
-            if (BF16 && !w.o_float) reinterpret_cast<__bf16*>(out)[c] = (__bf16)0.f;
+            if constexpr (BF16) reinterpret_cast<__bf16*>(out)[c] = (__bf16)0.f;
             else reinterpret_cast<float*>(out)[c] = 0.f;
         }
     }
@@ -122,12 +93,10 @@ __global__ __launch_bounds__(kThreads) void decay_rows_kernel(Walk w) {
 template <int D, bool BF16>
 void launch_rows(const Walk& w, hipStream_t stream) {
     const dim3 grid(w.B * w.H * (D / kSlice)), block(kThreads);
-    if (w.moment) hipLaunchKernelGGL((decay_rows_kernel<D, BF16, false, true>), grid, block, 0, stream, w);
-    else if (w.reverse) hipLaunchKernelGGL((decay_rows_kernel<D, BF16, true, false>), grid, block, 0, stream, w);
-    else hipLaunchKernelGGL((decay_rows_kernel<D, BF16, false, false>), grid, block, 0, stream, w);
+    hipLaunchKernelGGL((decay_rows_kernel<D, BF16>), grid, block, 0, stream, w);
 }
 
-__global__ __launch_bounds__(64) void moment_sum_kernel(const float* __restrict__ m, int B, int H, int slices, float* dlog) {
+__global__ __launch_bounds__(64) void moment_sum_kernel(const double* __restrict__ m, int B, int H, int slices, float* dlog) {
     const int h = blockIdx.x;
     double s = 0.;
     for (int i = threadIdx.x; i < B * slices; i += 64) s += m[((size_t)(i / slices) * H + h) * slices + i % slices];
@@ -158,9 +127,7 @@ __global__ __launch_bounds__(256) void share_sum_kernel(const float* __restrict_
 
 }  // namespace
 
-int decay_slices(int D) { return D / kSlice; }
-
-hipError_t launch_decay_walk(const Walk& w, hipStream_t stream) {
+hipError_t launch_decay_rows(const Walk& w, hipStream_t stream) {
     switch (w.D) {
         case 64: w.bf16 ? launch_rows<64, true>(w, stream) : launch_rows<64, false>(w, stream); break;
         case 128: w.bf16 ? launch_rows<128, true>(w, stream) : launch_rows<128, false>(w, stream); break;
@@ -170,7 +137,7 @@ hipError_t launch_decay_walk(const Walk& w, hipStream_t stream) {
     return hipGetLastError();
 }
 
-hipError_t launch_moment_sum(const float* moments, int B, int H, int slices, float* dlog, hipStream_t stream) {
+hipError_t launch_moment_sum(const double* moments, int B, int H, int slices, float* dlog, hipStream_t stream) {
     hipLaunchKernelGGL(moment_sum_kernel, dim3(H), dim3(64), 0, stream, moments, B, H, slices, dlog);
     return hipGetLastError();
 }

@@ -1,0 +1,619 @@
+// Linear attention with a decay for each head, in chunks of C rows on the matrix unit.  With local rows i = 0 .. C-1 and
+// the state S in front of them (sequence.h: pre = 1 forward, 0 in reverse):
+//   O = diag(g^(i+pre)) Q S + ((Q K^T) o M) V,   M_ij = g^(i-j) for j <= i,  0 else
+//   S <- g^C S + K^T diag(g^(C-pre-j)) V
+// A workgroup of four waves holds W columns of S in registers, a quarter per wave, and walks over the rows of one part of
+// one user's sequence for one head.  Everything is formed transposed (O^T = S^T Q^T + V^T P^T): a lane's entries of S, eight
+// of one column, are then an operand of the matrix instruction as they stand, and so are K^T and V from the transposing LDS
+// read; only P = Q K^T o M goes through LDS, each wave forming a share of it.
+//
+// Precision.  Sums and S are float.  The matrix unit takes bf16, so a float operand is cut into bf16 terms that add up to it:
+// three (24 bits) where the sum stays float - the state - and for float inputs, whose products take the six pairs of terms
+// above 2^-24; two (16 bits) for S and P where the result is rounded to bf16 anyway (2^-8).  g^C S is S + (g^C - 1) S, so that
+// the error of a rounded g^C does not add up over the chunks.
+#include "kernels.h"
+#include "sequence.h"
+
+namespace solar {
+
+namespace {
+
+constexpr int kThreads = 256;
+
+typedef __bf16 v4bf __attribute__((ext_vector_type(4)));
+
+template <int D, bool BF16, bool MOMENT>
+struct ChunkCfg {
+    static constexpr int C = BF16 && D <= 128 && !MOMENT ? 64 : 32;     // rows of a chunk
+    static constexpr int W = BF16 && D == 128 && !MOMENT ? 128 : 64;    // columns of S per workgroup
+    static constexpr int NB = W / 64;                                   // tiles of 16 columns per wave
+    static constexpr int NT = BF16 ? 1 : 3;                             // terms of an input
+    static constexpr int TP = BF16 && !MOMENT ? 2 : 3;                  // terms of P and S where they meet V and Q
+    static constexpr int kWaves = D == 256 && (MOMENT || !BF16) ? 1 : 2;   // per SIMD: S and T alone take 128 registers there
+    static constexpr int LD = D + 8, LW = W + 8, LP = C + 8;            // bf16 per row of the images
+    static constexpr int kQ = NT * C * LD, kV = NT * C * LW, kP = TP * C * LP;
+    static constexpr size_t lds_bytes(bool out) { return 2 * (size_t)(kQ + kV + (out ? kQ + kP : 0)) + 4 * 2 * (C + 1); }
+};
+
+// x = the sum of its terms, to 8 bits each
+template <int T>
+__device__ __forceinline__ void split(const float (&x)[8], v8bf (&s)[T]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        float r = x[i];
+#pragma unroll
+        for (int k = 0; k < T; ++k) {
+            s[k][i] = (__bf16)r;
+            if (k + 1 < T) r -= (float)s[k][i];
+        }
+    }
+}
+
+__device__ __forceinline__ v4f mfma(v8bf a, v8bf b, v4f c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+
+// c + a b over the pairs of terms that matter, the small ones first
+template <int TA, int TB>
+__device__ __forceinline__ v4f product(const v8bf (&a)[TA], const v8bf (&b)[TB], v4f c) {
+    constexpr int T = TA > TB ? TA : TB;
+#pragma unroll
+    for (int sum = T - 1; sum >= 0; --sum)
+#pragma unroll
+        for (int i = 0; i < TA; ++i)
+            if (sum - i >= 0 && sum - i < TB) c = mfma(a[i], b[sum - i], c);
+    return c;
+}
+
+__device__ __forceinline__ v8bf lds8(const __bf16* p) { return *reinterpret_cast<const v8bf*>(p); }
+
+// Transposing read of 16-bit elements from rows r .. r+7 of an LDS image: lane i of a group of 16 passes the address of four
+// elements in row i/4 and receives element i%4 of the lanes i/4, 4 + i/4, 8 + i/4, 12 + i/4: rows 0..3 of "its" column.
+__device__ __forceinline__ v8bf lds_turned(const __bf16* p, int four_rows) {
+    typedef short v4s __attribute__((ext_vector_type(4)));
+    typedef __attribute__((address_space(3))) v4s* lds_ptr;
+    const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(p));
+    const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(p + four_rows));
+    typedef short v8s __attribute__((ext_vector_type(8)));
+    const v8s r = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+    return __builtin_bit_cast(v8bf, r);
+}
+
+// Rows of one tensor, head and user in the order of the walk.  Addresses are a uniform base and a 32-bit offset per lane: row
+// i of the chunk that starts at row `done` is at(done) + off(i), at() lying below all rows of the chunk.
+struct Rows {
+    const char* first;
+    int64_t step;       // bytes; |step| * 64 < 2^31 by the host's checks
+    int64_t low;        // of the last row of a chunk where the walk goes down
+
+    template <int C>
+    __device__ __forceinline__ static Rows make(const char* first, int64_t step) { return {first, step, step < 0 ? (C - 1) * step : 0}; }
+    __device__ __forceinline__ const char* at(int done) const { return first + done * step + low; }
+    __device__ __forceinline__ uint32_t off(int i) const { return (uint32_t)(i * (int)step - (int)low); }
+};
+
+// One thread's share of the rows of a chunk on their way from memory to LDS: vectors of eight elements.
+template <int C, int COLS, bool BF16>
+struct Fetch {
+    static constexpr int PER = COLS / 8, N = C * PER / kThreads, VS = BF16 ? 1 : 2;
+    v4u x[N][VS];
+
+    // rows i < cnt come from memory, the others are zero
+    __device__ __forceinline__ void load(const Rows& r, int done, int cnt) {
+        const char* p = r.at(done);
+        const int i0 = threadIdx.x / PER, c = threadIdx.x % PER;
+        // the offset holds `low`, which the whole chunk shares: p + u down + off + 16 v is in row i0 + u (kThreads / PER)
+        const uint32_t off = r.off(i0) + c * VS * 16;
+        const int64_t down = (int64_t)(kThreads / PER) * r.step;
+        if (cnt >= C) {
+#pragma unroll
+            for (int u = 0; u < N; ++u)
+#pragma unroll
+                for (int v = 0; v < VS; ++v) x[u][v] = *reinterpret_cast<const v4u*>(p + u * down + (off + v * 16));
+        } else {
+#pragma unroll
+            for (int u = 0; u < N; ++u)
+#pragma unroll
+                for (int v = 0; v < VS; ++v) {
+                    x[u][v] = v4u{0u, 0u, 0u, 0u};
+                    if (i0 + u * (kThreads / PER) < cnt)
+                        x[u][v] = *reinterpret_cast<const v4u*>(p + u * down + (off + v * 16));
+                }
+        }
+    }
+
+    __device__ __forceinline__ void store(__bf16* img, int ld) const {
+#pragma unroll
+        for (int u = 0; u < N; ++u) {
+            const int at = threadIdx.x + u * kThreads, i = at / PER, c = at % PER;
+            __bf16* to = img + i * ld + 8 * c;
+            if constexpr (BF16) {
+                *reinterpret_cast<v4u*>(to) = x[u][0];
+            } else {
+                float f[8];
+                v8bf s[3];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) f[e] = __uint_as_float(x[u][e / 4][e % 4]);
+                split<3>(f, s);
+#pragma unroll
+                for (int k = 0; k < 3; ++k) *reinterpret_cast<v8bf*>(to + k * C * ld) = s[k];
+            }
+        }
+    }
+};
+
+// kOut: outputs; kState: the state behind each part but the last, from a zero state, into w.parts; kMoment: the derivative of
+// the outputs by log g, summed against their gradient; kMomentState: kState, and the derivative of these states; kLast: the
+// state behind the last part, where nobody wants outputs.
+enum { kOut, kState, kMoment, kMomentState, kLast };
+
+template <int D, bool BF16, int MODE>
+__global__ __launch_bounds__(kThreads, (ChunkCfg<D, BF16, MODE == kMoment || MODE == kMomentState>::kWaves)) void decay_chunk_kernel(Walk w) {
+    constexpr bool MOMENT = MODE == kMoment || MODE == kMomentState, STATES = MODE == kState || MODE == kMomentState;
+    constexpr bool OUT = MODE == kOut || MODE == kMoment;
+    using F = ChunkCfg<D, BF16, MOMENT>;
+    constexpr int C = F::C, W = F::W, NB = F::NB, NT = F::NT, TP = F::TP, LD = F::LD, LW = F::LW, LP = F::LP;
+    constexpr int NS = D / W, NJ = D / 32, NC = C / 16, NK = C / 32, ES = BF16 ? 2 : 4;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    __bf16* const ki = reinterpret_cast<__bf16*>(lds);                  // [NT][C][LD]
+    __bf16* const vi = ki + F::kQ;                                      // [NT][C][LW]
+    __bf16* const qi = vi + F::kV;                                      // [NT][C][LD]
+    __bf16* const pi = qi + (OUT ? F::kQ : 0);                          // [TP][C][LP]: row t, column s
+    float* const pw = reinterpret_cast<float*>(pi + (OUT ? F::kP : 0)); // g^n, n = 0 .. C
+    float* const pk = pw + C + 1;                                       // kv_scale g^n
+
+    // Slices of one part and heads that share K and V run on one XCD (workgroups go to the eight in turn), where they
+    // find each other's rows in its L2.
+    const int share = w.k.share, nparts = MODE == kLast ? 1 : STATES ? w.nparts - 1 : w.nparts;
+    const int turn = blockIdx.x >> 3, slice = turn % NS, k0 = turn / NS;
+    const int64_t unit = (int64_t)(k0 / share * 8 + (blockIdx.x & 7)) * share + k0 % share;
+    if (unit >= (int64_t)w.B * w.H * nparts) return;
+    const int h = (int)(unit % w.H), b = (int)(unit / w.H / nparts);
+    // in the order of the walk; the last part's state is nobody's start
+    const int order = MODE == kLast ? w.nparts - 1 : (int)(unit / w.H % nparts), part = w.reverse ? w.nparts - 1 - order : order;
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, c16 = lane & 15, g4 = lane >> 4;
+    const int len = user_len(w.lengths, b, w.N);
+    const int row0 = part * w.part_rows;                                // may not overflow: part < nparts
+    const int rows = w.N - row0 < w.part_rows ? w.N - row0 : w.part_rows;
+    const int count = len - row0 < 0 ? 0 : (len - row0 < rows ? len - row0 : rows);
+    const int pre = w.reverse ? 0 : 1;
+    const float lg = w.log_decay[h];
+    const int col0 = slice * W;                                         // this workgroup's columns of S
+    const int mycol = col0 + wave * 16 * NB;                            // this wave's
+
+    for (int n = tid; n <= C; n += kThreads) {
+        const float x = n ? expf(lg * (float)n) : 1.f;                  // log g may be -infinity
+        pw[n] = x;
+        pk[n] = w.kv_scale * x;
+    }
+
+    // S[nb][j][a]: rows 32 j + 8 g4 + 4 a + (0..3), column mycol + 16 nb + c16
+    v4f S[NB][NJ][2], T[MOMENT ? NB : 1][MOMENT ? NJ : 1][2];
+    const size_t state_at = ((size_t)b * w.H + h) * D * D;
+    const size_t part_at = (((size_t)b * w.H + h) * (w.nparts - 1) + (order - 1)) * D * D;   // order > 0 only
+    const float* start = w.nparts == 1 || order == 0 ? (w.state_in ? w.state_in + state_at : nullptr) : w.parts + part_at;
+    const bool turned = order == 0 && w.in_turned;
+    if (STATES) start = nullptr;
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
+#pragma unroll
+            for (int a = 0; a < 2; ++a)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int r = 32 * j + 8 * g4 + 4 * a + i, col = mycol + 16 * nb + c16;
+                    S[nb][j][a][i] = start ? start[turned ? (size_t)col * D + r : (size_t)r * D + col] : 0.f;
+                    if constexpr (MOMENT)
+                        T[nb][j][a][i] = MODE == kMoment && order > 0 ? w.part_moments[part_at + (size_t)r * D + col] : 0.f;
+                }
+
+    const int64_t step = w.reverse ? -1 : 1;
+    const int64_t first = w.reverse ? row0 + (int64_t)count - 1 : row0;
+    const Rows kr = Rows::make<C>(row_of(w.k, b, first, h), step * w.k.s.row);
+    const Rows vr = Rows::make<C>(row_of(w.v, b, first, h) + (size_t)col0 * ES, step * w.v.s.row);
+    Rows qr = kr, outr = kr;                                            // of q, and of o or the gradient
+    if constexpr (OUT) qr = Rows::make<C>(row_of(w.q, b, first, h), step * w.q.s.row);
+    if constexpr (MODE == kOut) outr = Rows::make<C>(row_of(w.o, b, first, h), step * w.o.s.row);
+    if constexpr (MODE == kMoment) outr = Rows::make<C>(row_of(w.grad, b, first, h), step * w.grad.s.row);
+    Fetch<C, D, BF16> fq, fk;
+    Fetch<C, W, BF16> fv;
+    auto fetch = [&](int done) __attribute__((always_inline)) {
+        const int cnt = count - done;
+        fk.load(kr, done, cnt);
+        fv.load(vr, done, cnt);
+        if constexpr (OUT) fq.load(qr, done, cnt);
+    };
+    if (count) fetch(0);
+    double z = 0.;          // terms of either sign over thousands of rows
+
+    for (int done = 0; done < count; done += C) {
+        const int cnt = count - done < C ? count - done : C;
+        fk.store(ki, LD);
+        fv.store(vi, LW);
+        if constexpr (OUT) fq.store(qi, LD);
+        __syncthreads();
+        if (done + C < count) fetch(done + C);
+
+        v4f O[NB][NC];
+        // Q S, times g^(i+pre)
+        auto from_state = [&]() __attribute__((always_inline)) {
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                for (int t = 0; t < NC; ++t) O[nb][t] = v4f{0.f, 0.f, 0.f, 0.f};
+            v4f R[MOMENT ? NB : 1][NC];
+            if constexpr (MOMENT)
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                    for (int t = 0; t < NC; ++t) R[nb][t] = v4f{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) {
+                v8bf s[NB][TP], m[MOMENT ? NB : 1][TP];
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) {
+                    float x[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) x[e] = S[nb][j][e / 4][e % 4];
+                    split<TP>(x, s[nb]);
+                    if constexpr (MOMENT) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) x[e] = T[nb][j][e / 4][e % 4];
+                        split<TP>(x, m[nb]);
+                    }
+                }
+#pragma unroll
+                for (int t = 0; t < NC; ++t) {
+                    v8bf q[NT];
+#pragma unroll
+                    for (int k = 0; k < NT; ++k) q[k] = lds8(qi + (k * C + 16 * t + c16) * LD + 32 * j + 8 * g4);
+#pragma unroll
+                    for (int nb = 0; nb < NB; ++nb) {
+                        O[nb][t] = product<TP, NT>(s[nb], q, O[nb][t]);
+                        if constexpr (MOMENT) R[nb][t] = product<TP, NT>(m[nb], q, R[nb][t]);
+                    }
+                }
+                // or the operands of all steps are read at once, and registers spilled
+                __builtin_amdgcn_sched_barrier(0);
+            }
+#pragma unroll
+            for (int t = 0; t < NC; ++t) {
+                const int i = 16 * t + c16;
+                const float x = pw[i + pre];
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) {
+                    if constexpr (MOMENT) O[nb][t] = (R[nb][t] + (float)(i + 1) * O[nb][t]) * x;
+                    else O[nb][t] *= x;
+                }
+            }
+        };
+
+        if constexpr (OUT) {
+            // P^T, rows s, columns t: wave t0 takes the tiles of columns t0, where there are as many waves as tiles; with two
+            // tiles, the three below the diagonal go to three waves
+            auto tile = [&](int sb, int tb) __attribute__((always_inline)) {
+                v4f p = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int j = 0; j < NJ; ++j) {
+                    v8bf a[NT], q[NT];
+#pragma unroll
+                    for (int k = 0; k < NT; ++k) {
+                        a[k] = lds8(ki + (k * C + 16 * sb + c16) * LD + 32 * j + 8 * g4);
+                        q[k] = lds8(qi + (k * C + 16 * tb + c16) * LD + 32 * j + 8 * g4);
+                    }
+                    p = product<NT, NT>(a, q, p);
+                }
+                v4bf term[TP];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int ago = 16 * (tb - sb) + c16 - 4 * g4 - i;
+                    const float wgt = MOMENT ? pk[ago < 0 ? 0 : ago] * (float)ago : pk[ago < 0 ? 0 : ago];
+                    float x = ago < 0 ? 0.f : p[i] * wgt;       // not 0 * p: rows after t may hold anything
+#pragma unroll
+                    for (int k = 0; k < TP; ++k) {
+                        term[k][i] = (__bf16)x;
+                        if (k + 1 < TP) x -= (float)term[k][i];
+                    }
+                }
+#pragma unroll
+                for (int k = 0; k < TP; ++k)
+                    *reinterpret_cast<v4bf*>(pi + (k * C + 16 * tb + c16) * LP + 16 * sb + 4 * g4) = term[k];
+            };
+            auto none = [&](int sb, int tb) __attribute__((always_inline)) {
+#pragma unroll
+                for (int k = 0; k < TP; ++k)
+                    *reinterpret_cast<uint2*>(pi + (k * C + 16 * tb + c16) * LP + 16 * sb + 4 * g4) = make_uint2(0u, 0u);
+            };
+            if constexpr (NC == 4) {
+#pragma unroll 1
+                for (int sb = 0; sb <= wave; ++sb) tile(sb, wave);
+                if (!(wave & 1)) none(wave + 1, wave);          // the columns of V come in 32 rows
+            } else {
+                if (wave < 3) tile(wave >> 1, (wave + 1) >> 1);
+                else none(1, 0);
+            }
+            from_state();
+            __syncthreads();
+        }
+
+        // V's rows 32 kk + 8 g4 + (0..7) of this wave's columns
+        auto column = [&](int nb, int kk, v8bf (&v)[NT]) __attribute__((always_inline)) {
+#pragma unroll
+            for (int k = 0; k < NT; ++k)
+                v[k] = lds_turned(vi + (k * C + 32 * kk + 8 * g4 + (c16 >> 2)) * LW + wave * 16 * NB + 16 * nb + 4 * (c16 & 3), 4 * LW);
+        };
+        if constexpr (OUT) {
+#pragma unroll
+            for (int kk = 0; kk < NK; ++kk) {
+                v8bf v[NB][NT];
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) column(nb, kk, v[nb]);
+#pragma unroll
+                for (int t = 2 * kk; t < NC; ++t) {
+                    v8bf p[TP];
+#pragma unroll
+                    for (int k = 0; k < TP; ++k) p[k] = lds8(pi + (k * C + 16 * t + c16) * LP + 32 * kk + 8 * g4);
+#pragma unroll
+                    for (int nb = 0; nb < NB; ++nb) O[nb][t] = product<NT, TP>(v[nb], p, O[nb][t]);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            // A row of V that is not finite reaches the rows before it here, as 0 * V.  Then the products are taken again with
+            // zeros for such values, and a column that has met one by row t is NaN from there on: the same products count them.
+            float probe = 0.f;
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                for (int t = 0; t < NC; ++t)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) probe = fmaf(O[nb][t][i], 0.f, probe);
+            __builtin_amdgcn_sched_barrier(0);
+            if (__builtin_expect(__any(probe != 0.f), 0)) {
+                from_state();
+#pragma unroll
+                for (int t = 0; t < NC; ++t)
+#pragma unroll
+                    for (int nb = 0; nb < NB; ++nb) {
+                        v4f met = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                        for (int kk = 0; kk <= t / 2; ++kk) {
+                            v8bf v[NT], p[TP], bad, upto;
+                            column(nb, kk, v);
+#pragma unroll
+                            for (int k = 0; k < TP; ++k) p[k] = lds8(pi + (k * C + 16 * t + c16) * LP + 32 * kk + 8 * g4);
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) {
+                                bool fine = true;
+#pragma unroll
+                                for (int k = 0; k < NT; ++k) {
+                                    const bool f = finite32((float)v[k][e]);
+                                    fine = fine && f;
+                                    if (!f) v[k][e] = (__bf16)0.f;
+                                }
+                                bad[e] = fine ? (__bf16)0.f : (__bf16)1.f;
+                                upto[e] = 32 * kk + 8 * g4 + e <= 16 * t + c16 ? (__bf16)1.f : (__bf16)0.f;
+                            }
+                            O[nb][t] = product<NT, TP>(v, p, O[nb][t]);
+                            met = mfma(bad, upto, met);
+                            __builtin_amdgcn_sched_barrier(0);
+                        }
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            if (met[i] != 0.f) O[nb][t][i] = __builtin_nanf("");
+                    }
+            }
+            float zc = 0.f;
+            const char* const outp = outr.at(done);
+#pragma unroll
+            for (int t = 0; t < NC; ++t) {
+                const int i = 16 * t + c16;
+                const uint32_t row = outr.off(i);
+                if (i < cnt)
+#pragma unroll
+                    for (int nb = 0; nb < NB; ++nb) {
+                        const v4f x = O[nb][t] * w.o_scale;
+                        const int col = mycol + 16 * nb + 4 * g4;
+                        if constexpr (MODE == kMoment) {
+                            const char* p = outp + (row + col * ES);
+                            v4f d;
+                            if constexpr (BF16) {
+                                const uint2 u = *reinterpret_cast<const uint2*>(p);
+                                d = v4f{bf16_lo(u.x), bf16_hi(u.x), bf16_lo(u.y), bf16_hi(u.y)};
+                            } else {
+                                d = *reinterpret_cast<const v4f*>(p);
+                            }
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) zc = fmaf(x[e], d[e], zc);
+                        } else {
+                            char* p = const_cast<char*>(outp);
+                            if (BF16 && !w.o_float) {
+                                const v4bf y = {(__bf16)x[0], (__bf16)x[1], (__bf16)x[2], (__bf16)x[3]};
+                                *reinterpret_cast<v4bf*>(p + (row + col * 2)) = y;
+                            } else {
+                                *reinterpret_cast<v4f*>(p + (row + col * 4)) = x;
+                            }
+                        }
+                    }
+            }
+            if constexpr (MODE == kMoment) z += zc;
+        }
+
+        // S <- g^cnt S + K^T diag(g^(cnt-pre-j)) V, and T <- g^cnt (T + cnt S) + ... with the weights' derivative
+        const float gc = expm1f(lg * (float)cnt);
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+            for (int j = 0; j < NJ; ++j)
+#pragma unroll
+                for (int a = 0; a < 2; ++a)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        if constexpr (MOMENT) {
+                            const float x = fmaf((float)cnt, S[nb][j][a][i], T[nb][j][a][i]);
+                            T[nb][j][a][i] = fmaf(x, gc, x);
+                        }
+                        S[nb][j][a][i] = fmaf(S[nb][j][a][i], gc, S[nb][j][a][i]);
+                    }
+#pragma unroll
+        for (int kk = 0; kk < NK; ++kk) {
+            v8bf v[NB][3], m[MOMENT ? NB : 1][3];
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) {
+                v8bf raw[NT];
+                column(nb, kk, raw);
+                float x[8], y[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const int left = cnt - pre - (32 * kk + 8 * g4 + e);    // below 0 only for rows past the last, zero in LDS
+                    float f = (float)raw[NT - 1][e];
+#pragma unroll
+                    for (int k = NT - 2; k >= 0; --k) f += (float)raw[k][e];
+                    x[e] = f * pk[left < 0 ? 0 : left];
+                    if constexpr (MOMENT) y[e] = x[e] * (float)left;
+                }
+                split<3>(x, v[nb]);
+                if constexpr (MOMENT) split<3>(y, m[nb]);
+            }
+#pragma unroll
+            for (int j = 0; j < NJ; ++j)
+#pragma unroll
+                for (int a = 0; a < 2; ++a) {
+                    v8bf kt[NT];
+#pragma unroll
+                    for (int k = 0; k < NT; ++k)
+                        kt[k] = lds_turned(ki + (k * C + 32 * kk + 8 * g4 + (c16 >> 2)) * LD + 32 * j + 4 * a + 8 * (c16 & 3), 4 * LD);
+#pragma unroll
+                    for (int nb = 0; nb < NB; ++nb) {
+                        S[nb][j][a] = product<NT, 3>(kt, v[nb], S[nb][j][a]);
+                        if constexpr (MOMENT) T[nb][j][a] = product<NT, 3>(kt, m[nb], T[nb][j][a]);
+                    }
+                    if (a && (j & 1)) __builtin_amdgcn_sched_barrier(0);
+                }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        __syncthreads();        // everybody is done with the images
+    }
+
+    if constexpr (MODE == kOut) {
+        // rows of this part that are not valid
+        const int es = BF16 && !w.o_float ? 2 : 4, vecs = W * es / 16;
+        for (int i = tid; i < (rows - count) * vecs; i += kThreads) {
+            char* p = row_of(w.o, b, row0 + count + i / vecs, h) + (size_t)col0 * es + i % vecs * 16;
+            *reinterpret_cast<v4u*>(p) = v4u{0u, 0u, 0u, 0u};
+        }
+    }
+    float* to = nullptr;
+    if (STATES) to = w.parts + (((size_t)b * w.H + h) * (w.nparts - 1) + order) * D * D;
+    else if (MODE != kMoment && order == w.nparts - 1 && w.state_out) to = w.state_out + state_at;
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
+#pragma unroll
+            for (int a = 0; a < 2; ++a)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const size_t at = (size_t)(32 * j + 8 * g4 + 4 * a + i) * D + mycol + 16 * nb + c16;
+                    if (to) to[at] = S[nb][j][a][i];
+                    if constexpr (MODE == kMomentState)
+                        w.part_moments[(((size_t)b * w.H + h) * (w.nparts - 1) + order) * D * D + at] = T[nb][j][a][i];
+                    if constexpr (MODE == kMoment)
+                        if (order == w.nparts - 1 && w.grad_state) z += (double)w.grad_state[state_at + at] * T[nb][j][a][i];
+                }
+    if constexpr (MODE == kMoment) {
+#pragma unroll
+        for (int m = 32; m; m >>= 1) z += __shfl_xor(z, m);
+        __syncthreads();        // the images are done with, and a part without rows has not come by a barrier
+        double* const sum = reinterpret_cast<double*>(lds);
+        if (lane == 0) sum[wave] = z;
+        __syncthreads();
+        if (tid == 0) w.moments[(((size_t)b * w.H + h) * w.nparts + part) * NS + slice] = sum[0] + sum[1] + sum[2] + sum[3];
+    }
+}
+
+// parts[o] holds the state behind part o of the walk from a zero state; it becomes the state behind parts 0 .. o from
+// state_in, which is the start of part o + 1.
+template <bool MOMENT>
+__global__ __launch_bounds__(kThreads) void join_parts_kernel(Walk w) {
+    const int DD = w.D * w.D;
+    const size_t i = (size_t)blockIdx.x * kThreads + threadIdx.x;       // an element of a state
+    const int e = (int)(i % DD), h = (int)(i / DD % w.H), b = (int)(i / DD / w.H);
+    const int len = user_len(w.lengths, b, w.N);
+    const float lg = w.log_decay[h];
+    const size_t bh = (size_t)b * w.H + h;
+    float s = 0.f, t = 0.f;
+    if (w.state_in) s = w.state_in[bh * DD + (w.in_turned ? (e % w.D) * w.D + e / w.D : e)];
+    float* p = w.parts + bh * (w.nparts - 1) * DD + e;
+    float* pm = MOMENT ? w.part_moments + bh * (w.nparts - 1) * DD + e : nullptr;
+    for (int o = 0; o + 1 < w.nparts; ++o) {
+        const int part = w.reverse ? w.nparts - 1 - o : o, row0 = part * w.part_rows;
+        const int rows = w.N - row0 < w.part_rows ? w.N - row0 : w.part_rows;
+        const int count = len - row0 < 0 ? 0 : (len - row0 < rows ? len - row0 : rows);
+        const float g = expm1f(lg * (float)count), gc = count ? g : 0.f;      // log g may be -infinity
+        if constexpr (MOMENT) {
+            const float x = fmaf((float)count, s, t);
+            t = fmaf(x, gc, x) + pm[(size_t)o * DD];
+            pm[(size_t)o * DD] = t;
+        }
+        s = fmaf(s, gc, s) + p[(size_t)o * DD];
+        p[(size_t)o * DD] = s;
+    }
+}
+
+template <int D, bool BF16, int MODE>
+hipError_t launch(const Walk& w, int parts, hipStream_t stream) {
+    using F = ChunkCfg<D, BF16, MODE == kMoment || MODE == kMomentState>;
+    auto kern = decay_chunk_kernel<D, BF16, MODE>;
+    constexpr size_t bytes = F::lds_bytes(MODE == kOut || MODE == kMoment);
+    hipError_t e = allow_dynamic_lds(reinterpret_cast<const void*>(kern), bytes);
+    if (e != hipSuccess) return e;
+    const int share = w.k.share;
+    const int64_t groups = (int64_t)w.B * w.H * parts / share;
+    const int64_t blocks = (groups + 7) / 8 * 8 * share * (D / F::W);
+    hipLaunchKernelGGL(kern, dim3((unsigned)blocks), dim3(kThreads), bytes, stream, w);
+    return hipGetLastError();
+}
+
+template <int D, bool BF16>
+hipError_t walk(const Walk& w, hipStream_t stream) {
+    hipError_t e;
+    if (w.nparts > 1) {
+        e = w.moment ? launch<D, BF16, kMomentState>(w, w.nparts - 1, stream) : launch<D, BF16, kState>(w, w.nparts - 1, stream);
+        if (e != hipSuccess) return e;
+        const dim3 grid((unsigned)((size_t)w.B * w.H * D * D / kThreads));
+        if (w.moment) hipLaunchKernelGGL(join_parts_kernel<true>, grid, dim3(kThreads), 0, stream, w);
+        else hipLaunchKernelGGL(join_parts_kernel<false>, grid, dim3(kThreads), 0, stream, w);
+        e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    if (!w.moment && !w.o.data) return launch<D, BF16, kLast>(w, 1, stream);
+    return w.moment ? launch<D, BF16, kMoment>(w, w.nparts, stream) : launch<D, BF16, kOut>(w, w.nparts, stream);
+}
+
+}  // namespace
+
+hipError_t launch_decay_chunks(const Walk& w, hipStream_t stream) {
+    switch (w.D) {
+        case 64: return w.bf16 ? walk<64, true>(w, stream) : walk<64, false>(w, stream);
+        case 128: return w.bf16 ? walk<128, true>(w, stream) : walk<128, false>(w, stream);
+        case 256: return w.bf16 ? walk<256, true>(w, stream) : walk<256, false>(w, stream);
+        default: return hipErrorInvalidValue;
+    }
+}
+
+int moment_slices(int D) { return D / 64; }
+
+// Parts that a sequence is cut into.  Two workgroups of the kernel fit a compute unit, so 512 fill the GPU; every part but
+// the last reads K and V once more, so there are no more than that takes, and none below eight chunks of 64 rows.
+DecayParts decay_parts(int B, int N, int H, int D, bool bf16) {
+    const int slices = bf16 && D == 128 ? 1 : D / 64;
+    const int64_t have = (int64_t)B * H * slices;
+    int64_t n = (512 + have - 1) / have;
+    const int64_t most = N / 512;
+    if (n > most) n = most;
+    if (n < 1) n = 1;
+    const int rows = (int)((((int64_t)N + n - 1) / n + 63) / 64 * 64);
+    return {ceil_div(N, rows), rows};
+}
+
+}  // namespace solar

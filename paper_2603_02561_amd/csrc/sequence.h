@@ -36,21 +36,34 @@ struct Walk {
     float o_scale, kv_scale;
     bool reverse, in_turned;        // in_turned: state_in is read transposed
     bool bf16, o_float;             // o_float: o is float whatever the inputs are
+    // the sequence is cut into nparts parts of part_rows rows (a multiple of 64); parts and part_moments are
+    // [B,H,nparts-1,D,D] work arrays, not used where nparts is 1
+    int nparts, part_rows;
+    float *parts, *part_moments;
     // the derivative by log g instead of o: `grad` is the gradient of o, `grad_state` of the last state (or null)
     bool moment;
     Heads grad;
     const float* grad_state;
-    float* moments;                 // [B][H][slices] partial sums
+    double* moments;                // [B][H][nparts][moment_slices(D)] partial sums
 };
 
 // decay.hip
-int decay_slices(int D);
-hipError_t launch_decay_walk(const Walk& w, hipStream_t stream);
+// A forward walk row by row, for a few rows (N <= kDecayRows); nparts is not looked at.
+constexpr int kDecayRows = 8;
+hipError_t launch_decay_rows(const Walk& w, hipStream_t stream);
 // dlog[h] = the sum of moments [B][H][slices] over users and slices
-hipError_t launch_moment_sum(const float* moments, int B, int H, int slices, float* dlog, hipStream_t stream);
+hipError_t launch_moment_sum(const double* moments, int B, int H, int slices, float* dlog, hipStream_t stream);
 // out [.., Hkv, D] = the sum of in [B,N,H,D] over the H / Hkv heads that share one
 hipError_t launch_share_sum(const float* in, int B, int N, int H, int Hkv, int D, const Heads& out, bool bf16,
                             hipStream_t stream);
+
+// decay_chunk.hip
+struct DecayParts {
+    int parts, rows;
+};
+DecayParts decay_parts(int B, int N, int H, int D, bool bf16);
+int moment_slices(int D);
+hipError_t launch_decay_chunks(const Walk& w, hipStream_t stream);
 
 // rotary.hip
 struct Rotary {
