@@ -73,7 +73,7 @@ struct DecayCarve {
     size_t total;
 };
 
-DecayCarve carve_decay(void* ws, int B, int N, int H, int Hkv, int D, bool bf16, bool backward) {
+DecayCarve carve_decay(void* ws, int B, int N, int H, int Hkv, int D, bool backward) {
     DecayCarve c = {};
     char* at = static_cast<char*>(ws);
     auto part = [&](size_t floats) {
@@ -82,7 +82,7 @@ DecayCarve carve_decay(void* ws, int B, int N, int H, int Hkv, int D, bool bf16,
         return p;
     };
     if (!backward && N <= kDecayRows) return c;
-    c.cut = decay_parts(B, N, H, D, bf16);
+    c.cut = decay_parts(B, N, H, D);
     const size_t states = (size_t)B * H * (c.cut.parts - 1) * D * D;
     c.parts = part(states);
     if (backward) {
@@ -162,7 +162,7 @@ solar_status solar_rotary(const void* Q, const void* K, const int32_t* lengths, 
 
 size_t solar_decay_workspace_bytes(int B, int N, int H, int Hkv, int D, solar_dtype t, int backward) {
     if (check_decay(B, N, H, Hkv, D, 1.f, t) != SOLAR_OK) return 0;
-    return carve_decay(nullptr, B, N, H, Hkv, D, t == SOLAR_BF16, backward != 0).total;
+    return carve_decay(nullptr, B, N, H, Hkv, D, backward != 0).total;
 }
 
 solar_status solar_decay_attention(const void* Q, const void* K, const void* V, const float* log_decay,
@@ -187,7 +187,7 @@ solar_status solar_decay_attention(const void* Q, const void* K, const void* V, 
         w.q = w.k;
     }
     if (!rows_near(w.k) || !rows_near(w.v) || !rows_near(w.q) || !rows_near(w.o)) return SOLAR_ERR_UNSUPPORTED;
-    const DecayCarve c = carve_decay(workspace, B, N, H, Hkv, D, t == SOLAR_BF16, false);
+    const DecayCarve c = carve_decay(workspace, B, N, H, Hkv, D, false);
     if (c.total && (!workspace || workspace_bytes < c.total || misaligned(workspace, 256))) return SOLAR_ERR_WORKSPACE;
     w.lengths = lengths;
     w.log_decay = log_decay;
@@ -227,7 +227,7 @@ solar_status solar_decay_attention_backward(const void* Q, const void* K, const 
     for (const Heads& x : {q, k, vv, g, dq, dk, dv})
         if (!rows_near(x)) return SOLAR_ERR_UNSUPPORTED;
     if ((int64_t)H * D > 1 << 22) return SOLAR_ERR_UNSUPPORTED;      // rows of the float work arrays
-    const DecayCarve c = carve_decay(workspace, B, N, H, Hkv, D, t == SOLAR_BF16, true);
+    const DecayCarve c = carve_decay(workspace, B, N, H, Hkv, D, true);
     if (c.total && (!workspace || workspace_bytes < c.total || misaligned(workspace, 256))) return SOLAR_ERR_WORKSPACE;
     if ((int64_t)B * N * Hkv * (D / 4) > kMaxBlocks * 256) return SOLAR_ERR_UNSUPPORTED;
     hipStream_t st = (hipStream_t)stream;

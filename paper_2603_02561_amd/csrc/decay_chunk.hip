@@ -2,7 +2,7 @@
 // the state S in front of them (sequence.h: pre = 1 forward, 0 in reverse):
 //   O = diag(g^(i+pre)) Q S + ((Q K^T) o M) V,   M_ij = g^(i-j) for j <= i,  0 else
 //   S <- g^C S + K^T diag(g^(C-pre-j)) V
-// A workgroup of four waves holds W columns of S in registers, a quarter per wave, and walks over the rows of one part of
+// A workgroup holds W columns of S in registers, sixteen per wave, and walks over the rows of one part of
 // one user's sequence for one head.  Everything is formed transposed (O^T = S^T Q^T + V^T P^T): a lane's entries of S, eight
 // of one column, are then an operand of the matrix instruction as they stand, and so are K^T and V from the transposing LDS
 // read; only P = Q K^T o M goes through LDS, each wave forming a share of it.
@@ -18,40 +18,77 @@ namespace solar {
 
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kJoinThreads = 256;
 
 typedef __bf16 v4bf __attribute__((ext_vector_type(4)));
 
 template <int D, bool BF16, bool MOMENT>
 struct ChunkCfg {
     static constexpr int C = BF16 && D <= 128 && !MOMENT ? 64 : 32;     // rows of a chunk
-    static constexpr int W = BF16 && D == 128 && !MOMENT ? 128 : 64;    // columns of S per workgroup
-    static constexpr int NB = W / 64;                                   // tiles of 16 columns per wave
+    static constexpr int W = D < 128 ? D : 128;                         // columns of S per workgroup, 16 per wave
+    static constexpr int kThreads = 4 * W;
     static constexpr int NT = BF16 ? 1 : 3;                             // terms of an input
     static constexpr int TP = BF16 && !MOMENT ? 2 : 3;                  // terms of P and S where they meet V and Q
-    static constexpr int kWaves = D == 256 && (MOMENT || !BF16) ? 1 : 2;   // per SIMD: S and T alone take 128 registers there
     static constexpr int LD = D + 8, LW = W + 8, LP = C + 8;            // bf16 per row of the images
     static constexpr int kQ = NT * C * LD, kV = NT * C * LW, kP = TP * C * LP;
-    static constexpr size_t lds_bytes(bool out) { return 2 * (size_t)(kQ + kV + (out ? kQ + kP : 0)) + 4 * 2 * (C + 1); }
+    static constexpr size_t lds_bytes(bool out) { return 2 * (size_t)(kQ + kV + (out ? kQ + kP : 0)) + 4 * (3 * C + 2); }
+    // Waves per SIMD that the registers are shared out for: two workgroups per compute unit where LDS has room for two and
+    // 128 registers hold what a wave needs.
+    static constexpr int waves(bool out) { return 2 * lds_bytes(out) <= 160 * 1024 && !(D == 256 || (MOMENT && D == 128)) ? W / 32 : W / 64; }
 };
+
+typedef float v8f __attribute__((ext_vector_type(8)));
+
+// The float that a bf16 stands for, from pairs in a register: converted one by one the compiler takes every conversion twice.
+__device__ __forceinline__ v8f widen(v8bf x) {
+    const v4u u = __builtin_bit_cast(v4u, x);
+    v8f f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        f[2 * e] = bf16_lo(u[e]);
+        f[2 * e + 1] = bf16_hi(u[e]);
+    }
+    return f;
+}
 
 // x = the sum of its terms, to 8 bits each
 template <int T>
-__device__ __forceinline__ void split(const float (&x)[8], v8bf (&s)[T]) {
+__device__ __forceinline__ void split(v8f x, v8bf (&s)[T]) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        float r = x[i];
-#pragma unroll
-        for (int k = 0; k < T; ++k) {
-            s[k][i] = (__bf16)r;
-            if (k + 1 < T) r -= (float)s[k][i];
-        }
+    for (int k = 0; k < T; ++k) {
+        s[k] = __builtin_convertvector(x, v8bf);
+        if (k + 1 < T) x -= widen(s[k]);
     }
 }
 
 __device__ __forceinline__ v4f mfma(v8bf a, v8bf b, v4f c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 
-// c + a b over the pairs of terms that matter, the small ones first
+// c[n] + a[n] b[n] over the pairs of terms that matter, the small ones first; the products that follow one another are
+// independent.  a or b is the same for all n.
+template <int N, int TA, int TB>
+__device__ __forceinline__ void products(const v8bf (&a)[TA], const v8bf (&b)[N][TB], v4f (&c)[N]) {
+    constexpr int T = TA > TB ? TA : TB;
+#pragma unroll
+    for (int sum = T - 1; sum >= 0; --sum)
+#pragma unroll
+        for (int i = 0; i < TA; ++i)
+            if (sum - i >= 0 && sum - i < TB)
+#pragma unroll
+                for (int n = 0; n < N; ++n) c[n] = mfma(a[i], b[n][sum - i], c[n]);
+}
+
+template <int N, int TA, int TB>
+__device__ __forceinline__ void products(const v8bf (&a)[N][TA], const v8bf (&b)[TB], v4f (&c)[N]) {
+    constexpr int T = TA > TB ? TA : TB;
+#pragma unroll
+    for (int sum = T - 1; sum >= 0; --sum)
+#pragma unroll
+        for (int i = 0; i < TA; ++i)
+            if (sum - i >= 0 && sum - i < TB)
+#pragma unroll
+                for (int n = 0; n < N; ++n) c[n] = mfma(a[n][i], b[sum - i], c[n]);
+}
+
 template <int TA, int TB>
 __device__ __forceinline__ v4f product(const v8bf (&a)[TA], const v8bf (&b)[TB], v4f c) {
     constexpr int T = TA > TB ? TA : TB;
@@ -91,50 +128,52 @@ struct Rows {
 };
 
 // One thread's share of the rows of a chunk on their way from memory to LDS: vectors of eight elements.
-template <int C, int COLS, bool BF16>
+template <int C, int COLS, int THREADS, bool BF16>
 struct Fetch {
-    static constexpr int PER = COLS / 8, N = C * PER / kThreads, VS = BF16 ? 1 : 2;
+    static constexpr int PER = COLS / 8, N = C * PER / THREADS, VS = BF16 ? 1 : 2;
     v4u x[N][VS];
 
-    // rows i < cnt come from memory, the others are zero
-    __device__ __forceinline__ void load(const Rows& r, int done, int cnt) {
+    // Row i is row done + i, or the last of the `count` rows where there are fewer: no branches, which would put the values
+    // into scratch memory.
+    __device__ __forceinline__ void load(const Rows& r, int done, int count) {
+        done = done < count ? done : count - 1;
         const char* p = r.at(done);
-        const int i0 = threadIdx.x / PER, c = threadIdx.x % PER;
-        // the offset holds `low`, which the whole chunk shares: p + u down + off + 16 v is in row i0 + u (kThreads / PER)
-        const uint32_t off = r.off(i0) + c * VS * 16;
-        const int64_t down = (int64_t)(kThreads / PER) * r.step;
-        if (cnt >= C) {
+        const int tid = fresh_tid(), i0 = tid / PER, c = tid % PER, last = count - 1 - done;
 #pragma unroll
-            for (int u = 0; u < N; ++u)
+        for (int u = 0; u < N; ++u) {
+            const int i = i0 + u * (THREADS / PER);
+            const uint32_t off = r.off(i < last ? i : last) + c * VS * 16;
 #pragma unroll
-                for (int v = 0; v < VS; ++v) x[u][v] = *reinterpret_cast<const v4u*>(p + u * down + (off + v * 16));
-        } else {
-#pragma unroll
-            for (int u = 0; u < N; ++u)
-#pragma unroll
-                for (int v = 0; v < VS; ++v) {
-                    x[u][v] = v4u{0u, 0u, 0u, 0u};
-                    if (i0 + u * (kThreads / PER) < cnt)
-                        x[u][v] = *reinterpret_cast<const v4u*>(p + u * down + (off + v * 16));
-                }
+            for (int v = 0; v < VS; ++v) x[u][v] = *reinterpret_cast<const v4u*>(p + (off + v * 16));
         }
     }
 
-    __device__ __forceinline__ void store(__bf16* img, int ld) const {
+    // to LDS, zeros for the rows from cnt on
+    __device__ __forceinline__ void store(__bf16* img, int ld, int cnt) const {
+        const int tid = fresh_tid();
 #pragma unroll
         for (int u = 0; u < N; ++u) {
-            const int at = threadIdx.x + u * kThreads, i = at / PER, c = at % PER;
+            const int at = tid + u * THREADS, i = at / PER, c = at % PER;
             __bf16* to = img + i * ld + 8 * c;
             if constexpr (BF16) {
                 *reinterpret_cast<v4u*>(to) = x[u][0];
             } else {
-                float f[8];
+                v8f f;
                 v8bf s[3];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) f[e] = __uint_as_float(x[u][e / 4][e % 4]);
                 split<3>(f, s);
 #pragma unroll
                 for (int k = 0; k < 3; ++k) *reinterpret_cast<v8bf*>(to + k * C * ld) = s[k];
+            }
+        }
+        if (cnt < C) {
+#pragma unroll
+            for (int u = 0; u < N; ++u) {
+                const int at = tid + u * THREADS, i = at / PER, c = at % PER;
+                if (i >= cnt)
+#pragma unroll
+                    for (int k = 0; k < (BF16 ? 1 : 3); ++k) *reinterpret_cast<v4u*>(img + (k * C + i) * ld + 8 * c) = v4u{0u, 0u, 0u, 0u};
             }
         }
     }
@@ -144,21 +183,23 @@ struct Fetch {
 // the outputs by log g, summed against their gradient; kMomentState: kState, and the derivative of these states; kLast: the
 // state behind the last part, where nobody wants outputs.
 enum { kOut, kState, kMoment, kMomentState, kLast };
+constexpr bool is_moment(int mode) { return mode == kMoment || mode == kMomentState; }
+constexpr bool is_out(int mode) { return mode == kOut || mode == kMoment; }
 
 template <int D, bool BF16, int MODE>
-__global__ __launch_bounds__(kThreads, (ChunkCfg<D, BF16, MODE == kMoment || MODE == kMomentState>::kWaves)) void decay_chunk_kernel(Walk w) {
-    constexpr bool MOMENT = MODE == kMoment || MODE == kMomentState, STATES = MODE == kState || MODE == kMomentState;
-    constexpr bool OUT = MODE == kOut || MODE == kMoment;
+__global__ __launch_bounds__((ChunkCfg<D, BF16, is_moment(MODE)>::kThreads), (ChunkCfg<D, BF16, is_moment(MODE)>::waves(is_out(MODE)))) void
+decay_chunk_kernel(Walk w) {
+    constexpr bool MOMENT = is_moment(MODE), OUT = is_out(MODE), STATES = MODE == kState || MODE == kMomentState;
     using F = ChunkCfg<D, BF16, MOMENT>;
-    constexpr int C = F::C, W = F::W, NB = F::NB, NT = F::NT, TP = F::TP, LD = F::LD, LW = F::LW, LP = F::LP;
-    constexpr int NS = D / W, NJ = D / 32, NC = C / 16, NK = C / 32, ES = BF16 ? 2 : 4;
+    constexpr int C = F::C, W = F::W, THREADS = F::kThreads, NT = F::NT, TP = F::TP, LD = F::LD, LW = F::LW, LP = F::LP;
+    constexpr int NW = THREADS / 64, NS = D / W, NJ = D / 32, NC = C / 16, NK = C / 32, ES = BF16 ? 2 : 4;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     __bf16* const ki = reinterpret_cast<__bf16*>(lds);                  // [NT][C][LD]
     __bf16* const vi = ki + F::kQ;                                      // [NT][C][LW]
     __bf16* const qi = vi + F::kV;                                      // [NT][C][LD]
     __bf16* const pi = qi + (OUT ? F::kQ : 0);                          // [TP][C][LP]: row t, column s
     float* const pw = reinterpret_cast<float*>(pi + (OUT ? F::kP : 0)); // g^n, n = 0 .. C
-    float* const pk = pw + C + 1;                                       // kv_scale g^n
+    float* const pk = pw + C + 1 + C;                                   // kv_scale g^n, n = -C .. C, zero below 0
 
     // Slices of one part and heads that share K and V run on one XCD (workgroups go to the eight in turn), where they
     // find each other's rows in its L2.
@@ -170,7 +211,8 @@ __global__ __launch_bounds__(kThreads, (ChunkCfg<D, BF16, MODE == kMoment || MOD
     // in the order of the walk; the last part's state is nobody's start
     const int order = MODE == kLast ? w.nparts - 1 : (int)(unit / w.H % nparts), part = w.reverse ? w.nparts - 1 - order : order;
 
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, c16 = lane & 15, g4 = lane >> 4;
+    const int tid = threadIdx.x, lane = tid & 63;
+    int wave = tid >> 6, c16 = lane & 15, g4 = lane >> 4;
     const int len = user_len(w.lengths, b, w.N);
     const int row0 = part * w.part_rows;                                // may not overflow: part < nparts
     const int rows = w.N - row0 < w.part_rows ? w.N - row0 : w.part_rows;
@@ -178,33 +220,40 @@ __global__ __launch_bounds__(kThreads, (ChunkCfg<D, BF16, MODE == kMoment || MOD
     const int pre = w.reverse ? 0 : 1;
     const float lg = w.log_decay[h];
     const int col0 = slice * W;                                         // this workgroup's columns of S
-    const int mycol = col0 + wave * 16 * NB;                            // this wave's
+    const int mycol = col0 + wave * 16;                            // this wave's
 
-    for (int n = tid; n <= C; n += kThreads) {
+    for (int n = tid; n <= C; n += THREADS) {
         const float x = n ? expf(lg * (float)n) : 1.f;                  // log g may be -infinity
         pw[n] = x;
         pk[n] = w.kv_scale * x;
+        if (n) pk[-n] = 0.f;
     }
 
-    // S[nb][j][a]: rows 32 j + 8 g4 + 4 a + (0..3), column mycol + 16 nb + c16
-    v4f S[NB][NJ][2], T[MOMENT ? NB : 1][MOMENT ? NJ : 1][2];
+    if constexpr (OUT) {
+        // P above the diagonal, as far as the 32 rows of V that a product takes reach: zero, and never written again
+        for (int n = tid; n < TP * C * 2; n += THREADS) {
+            const int t = n / 2 % C, k = n / 2 / C;
+            if (!(t & 16)) *reinterpret_cast<v4u*>(pi + (k * C + t) * LP + (t & ~15) + 16 + 8 * (n & 1)) = v4u{0u, 0u, 0u, 0u};
+        }
+    }
+
+    // S[j][a]: rows 32 j + 8 g4 + 4 a + (0..3), column mycol + c16
+    v4f S[NJ][2], T[MOMENT ? NJ : 1][2];
     const size_t state_at = ((size_t)b * w.H + h) * D * D;
     const size_t part_at = (((size_t)b * w.H + h) * (w.nparts - 1) + (order - 1)) * D * D;   // order > 0 only
     const float* start = w.nparts == 1 || order == 0 ? (w.state_in ? w.state_in + state_at : nullptr) : w.parts + part_at;
     const bool turned = order == 0 && w.in_turned;
     if (STATES) start = nullptr;
 #pragma unroll
-    for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
         for (int j = 0; j < NJ; ++j)
 #pragma unroll
             for (int a = 0; a < 2; ++a)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const int r = 32 * j + 8 * g4 + 4 * a + i, col = mycol + 16 * nb + c16;
-                    S[nb][j][a][i] = start ? start[turned ? (size_t)col * D + r : (size_t)r * D + col] : 0.f;
+                    const int r = 32 * j + 8 * g4 + 4 * a + i, col = mycol + c16;
+                    S[j][a][i] = start ? start[turned ? (size_t)col * D + r : (size_t)r * D + col] : 0.f;
                     if constexpr (MOMENT)
-                        T[nb][j][a][i] = MODE == kMoment && order > 0 ? w.part_moments[part_at + (size_t)r * D + col] : 0.f;
+                        T[j][a][i] = MODE == kMoment && order > 0 ? w.part_moments[part_at + (size_t)r * D + col] : 0.f;
                 }
 
     const int64_t step = w.reverse ? -1 : 1;
@@ -215,64 +264,55 @@ __global__ __launch_bounds__(kThreads, (ChunkCfg<D, BF16, MODE == kMoment || MOD
     if constexpr (OUT) qr = Rows::make<C>(row_of(w.q, b, first, h), step * w.q.s.row);
     if constexpr (MODE == kOut) outr = Rows::make<C>(row_of(w.o, b, first, h), step * w.o.s.row);
     if constexpr (MODE == kMoment) outr = Rows::make<C>(row_of(w.grad, b, first, h), step * w.grad.s.row);
-    Fetch<C, D, BF16> fq, fk;
-    Fetch<C, W, BF16> fv;
+    Fetch<C, D, THREADS, BF16> fq, fk;
+    Fetch<C, W, THREADS, BF16> fv;
     auto fetch = [&](int done) __attribute__((always_inline)) {
-        const int cnt = count - done;
-        fk.load(kr, done, cnt);
-        fv.load(vr, done, cnt);
-        if constexpr (OUT) fq.load(qr, done, cnt);
+        fk.load(kr, done, count);
+        fv.load(vr, done, count);
+        if constexpr (OUT) fq.load(qr, done, count);
     };
     if (count) fetch(0);
     double z = 0.;          // terms of either sign over thousands of rows
 
     for (int done = 0; done < count; done += C) {
         const int cnt = count - done < C ? count - done : C;
-        fk.store(ki, LD);
-        fv.store(vi, LW);
-        if constexpr (OUT) fq.store(qi, LD);
+        {   // addresses are formed anew for every chunk, not kept in registers by the dozen
+            const int t = fresh_tid();
+            wave = t >> 6, c16 = t & 15, g4 = t >> 4 & 3;
+        }
+        fk.store(ki, LD, cnt);
+        fv.store(vi, LW, cnt);
+        if constexpr (OUT) fq.store(qi, LD, cnt);
         __syncthreads();
-        if (done + C < count) fetch(done + C);
 
-        v4f O[NB][NC];
+        v4f O[NC];
         // Q S, times g^(i+pre)
         auto from_state = [&]() __attribute__((always_inline)) {
 #pragma unroll
-            for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-                for (int t = 0; t < NC; ++t) O[nb][t] = v4f{0.f, 0.f, 0.f, 0.f};
-            v4f R[MOMENT ? NB : 1][NC];
+                for (int t = 0; t < NC; ++t) O[t] = v4f{0.f, 0.f, 0.f, 0.f};
+            v4f R[NC];
             if constexpr (MOMENT)
 #pragma unroll
-                for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-                    for (int t = 0; t < NC; ++t) R[nb][t] = v4f{0.f, 0.f, 0.f, 0.f};
+                    for (int t = 0; t < NC; ++t) R[t] = v4f{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int j = 0; j < NJ; ++j) {
-                v8bf s[NB][TP], m[MOMENT ? NB : 1][TP];
+                v8bf s[TP], m[TP];
+                    v8f x;
 #pragma unroll
-                for (int nb = 0; nb < NB; ++nb) {
-                    float x[8];
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) x[e] = S[nb][j][e / 4][e % 4];
-                    split<TP>(x, s[nb]);
+                    for (int e = 0; e < 8; ++e) x[e] = S[j][e / 4][e % 4];
+                    split<TP>(x, s);
                     if constexpr (MOMENT) {
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) x[e] = T[nb][j][e / 4][e % 4];
-                        split<TP>(x, m[nb]);
+                        for (int e = 0; e < 8; ++e) x[e] = T[j][e / 4][e % 4];
+                        split<TP>(x, m);
                     }
-                }
+                v8bf q[NC][NT];
 #pragma unroll
-                for (int t = 0; t < NC; ++t) {
-                    v8bf q[NT];
+                for (int t = 0; t < NC; ++t)
 #pragma unroll
-                    for (int k = 0; k < NT; ++k) q[k] = lds8(qi + (k * C + 16 * t + c16) * LD + 32 * j + 8 * g4);
-#pragma unroll
-                    for (int nb = 0; nb < NB; ++nb) {
-                        O[nb][t] = product<TP, NT>(s[nb], q, O[nb][t]);
-                        if constexpr (MOMENT) R[nb][t] = product<TP, NT>(m[nb], q, R[nb][t]);
-                    }
-                }
+                    for (int k = 0; k < NT; ++k) q[t][k] = lds8(qi + (k * C + 16 * t + c16) * LD + 32 * j + 8 * g4);
+                products(s, q, O);
+                if constexpr (MOMENT) products(m, q, R);
                 // or the operands of all steps are read at once, and registers spilled
                 __builtin_amdgcn_sched_barrier(0);
             }
@@ -280,17 +320,13 @@ __global__ __launch_bounds__(kThreads, (ChunkCfg<D, BF16, MODE == kMoment || MOD
             for (int t = 0; t < NC; ++t) {
                 const int i = 16 * t + c16;
                 const float x = pw[i + pre];
-#pragma unroll
-                for (int nb = 0; nb < NB; ++nb) {
-                    if constexpr (MOMENT) O[nb][t] = (R[nb][t] + (float)(i + 1) * O[nb][t]) * x;
-                    else O[nb][t] *= x;
-                }
+                    if constexpr (MOMENT) O[t] = (R[t] + (float)(i + 1) * O[t]) * x;
+                    else O[t] *= x;
             }
         };
 
         if constexpr (OUT) {
-            // P^T, rows s, columns t: wave t0 takes the tiles of columns t0, where there are as many waves as tiles; with two
-            // tiles, the three below the diagonal go to three waves
+            // P^T, rows s, columns t, in tiles of 16: those up to the diagonal go round the waves
             auto tile = [&](int sb, int tb) __attribute__((always_inline)) {
                 v4f p = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -303,58 +339,53 @@ __global__ __launch_bounds__(kThreads, (ChunkCfg<D, BF16, MODE == kMoment || MOD
                     }
                     p = product<NT, NT>(a, q, p);
                 }
-                v4bf term[TP];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const int ago = 16 * (tb - sb) + c16 - 4 * g4 - i;
-                    const float wgt = MOMENT ? pk[ago < 0 ? 0 : ago] * (float)ago : pk[ago < 0 ? 0 : ago];
-                    float x = ago < 0 ? 0.f : p[i] * wgt;       // not 0 * p: rows after t may hold anything
-#pragma unroll
-                    for (int k = 0; k < TP; ++k) {
-                        term[k][i] = (__bf16)x;
-                        if (k + 1 < TP) x -= (float)term[k][i];
-                    }
+                    const float wgt = MOMENT ? pk[ago] * (float)ago : pk[ago];
+                    p[i] = ago < 0 ? 0.f : p[i] * wgt;          // not 0 * p: rows after t may hold anything
                 }
 #pragma unroll
-                for (int k = 0; k < TP; ++k)
-                    *reinterpret_cast<v4bf*>(pi + (k * C + 16 * tb + c16) * LP + 16 * sb + 4 * g4) = term[k];
+                for (int k = 0; k < TP; ++k) {
+                    const v4bf term = __builtin_convertvector(p, v4bf);
+                    *reinterpret_cast<v4bf*>(pi + (k * C + 16 * tb + c16) * LP + 16 * sb + 4 * g4) = term;
+                    if (k + 1 < TP) {
+                        const uint2 u = __builtin_bit_cast(uint2, term);
+                        p -= v4f{bf16_lo(u.x), bf16_hi(u.x), bf16_lo(u.y), bf16_hi(u.y)};
+                    }
+                }
             };
-            auto none = [&](int sb, int tb) __attribute__((always_inline)) {
-#pragma unroll
-                for (int k = 0; k < TP; ++k)
-                    *reinterpret_cast<uint2*>(pi + (k * C + 16 * tb + c16) * LP + 16 * sb + 4 * g4) = make_uint2(0u, 0u);
-            };
-            if constexpr (NC == 4) {
 #pragma unroll 1
-                for (int sb = 0; sb <= wave; ++sb) tile(sb, wave);
-                if (!(wave & 1)) none(wave + 1, wave);          // the columns of V come in 32 rows
-            } else {
-                if (wave < 3) tile(wave >> 1, (wave + 1) >> 1);
-                else none(1, 0);
+            for (int n = wave; n < NC * (NC + 1) / 2; n += NW) {
+                const int tb = n < 1 ? 0 : n < 3 ? 1 : n < 6 ? 2 : 3;
+                tile(n - tb * (tb + 1) / 2, tb);
             }
             from_state();
             __syncthreads();
         }
 
         // V's rows 32 kk + 8 g4 + (0..7) of this wave's columns
-        auto column = [&](int nb, int kk, v8bf (&v)[NT]) __attribute__((always_inline)) {
+        auto column = [&](int kk, v8bf (&v)[NT]) __attribute__((always_inline)) {
 #pragma unroll
             for (int k = 0; k < NT; ++k)
-                v[k] = lds_turned(vi + (k * C + 32 * kk + 8 * g4 + (c16 >> 2)) * LW + wave * 16 * NB + 16 * nb + 4 * (c16 & 3), 4 * LW);
+                v[k] = lds_turned(vi + (k * C + 32 * kk + 8 * g4 + (c16 >> 2)) * LW + wave * 16 + 4 * (c16 & 3), 4 * LW);
         };
         if constexpr (OUT) {
 #pragma unroll
             for (int kk = 0; kk < NK; ++kk) {
-                v8bf v[NB][NT];
+                v8bf v[NT];
+                column(kk, v);
+                // rows 32 kk of V meet the tiles of P from 2 kk on
+                v8bf p[2][TP];
 #pragma unroll
-                for (int nb = 0; nb < NB; ++nb) column(nb, kk, v[nb]);
+                for (int t2 = kk; t2 < NK; ++t2) {
 #pragma unroll
-                for (int t = 2 * kk; t < NC; ++t) {
-                    v8bf p[TP];
+                    for (int y = 0; y < 2; ++y)
 #pragma unroll
-                    for (int k = 0; k < TP; ++k) p[k] = lds8(pi + (k * C + 16 * t + c16) * LP + 32 * kk + 8 * g4);
-#pragma unroll
-                    for (int nb = 0; nb < NB; ++nb) O[nb][t] = product<NT, TP>(v[nb], p, O[nb][t]);
+                        for (int k = 0; k < TP; ++k) p[y][k] = lds8(pi + (k * C + 32 * t2 + 16 * y + c16) * LP + 32 * kk + 8 * g4);
+                    v4f o[2] = {O[2 * t2], O[2 * t2 + 1]};
+                    products(v, p, o);
+                    O[2 * t2] = o[0], O[2 * t2 + 1] = o[1];
                 }
                 __builtin_amdgcn_sched_barrier(0);
             }
@@ -362,23 +393,19 @@ __global__ __launch_bounds__(kThreads, (ChunkCfg<D, BF16, MODE == kMoment || MOD
             // zeros for such values, and a column that has met one by row t is NaN from there on: the same products count them.
             float probe = 0.f;
 #pragma unroll
-            for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
                 for (int t = 0; t < NC; ++t)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) probe = fmaf(O[nb][t][i], 0.f, probe);
+                    for (int i = 0; i < 4; ++i) probe = fmaf(O[t][i], 0.f, probe);
             __builtin_amdgcn_sched_barrier(0);
             if (__builtin_expect(__any(probe != 0.f), 0)) {
                 from_state();
 #pragma unroll
-                for (int t = 0; t < NC; ++t)
-#pragma unroll
-                    for (int nb = 0; nb < NB; ++nb) {
+                for (int t = 0; t < NC; ++t) {
                         v4f met = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                         for (int kk = 0; kk <= t / 2; ++kk) {
                             v8bf v[NT], p[TP], bad, upto;
-                            column(nb, kk, v);
+                            column(kk, v);
 #pragma unroll
                             for (int k = 0; k < TP; ++k) p[k] = lds8(pi + (k * C + 16 * t + c16) * LP + 32 * kk + 8 * g4);
 #pragma unroll
@@ -393,14 +420,14 @@ __global__ __launch_bounds__(kThreads, (ChunkCfg<D, BF16, MODE == kMoment || MOD
                                 bad[e] = fine ? (__bf16)0.f : (__bf16)1.f;
                                 upto[e] = 32 * kk + 8 * g4 + e <= 16 * t + c16 ? (__bf16)1.f : (__bf16)0.f;
                             }
-                            O[nb][t] = product<NT, TP>(v, p, O[nb][t]);
+                            O[t] = product<NT, TP>(v, p, O[t]);
                             met = mfma(bad, upto, met);
                             __builtin_amdgcn_sched_barrier(0);
                         }
 #pragma unroll
                         for (int i = 0; i < 4; ++i)
-                            if (met[i] != 0.f) O[nb][t][i] = __builtin_nanf("");
-                    }
+                            if (met[i] != 0.f) O[t][i] = __builtin_nanf("");
+                }
             }
             float zc = 0.f;
             const char* const outp = outr.at(done);
@@ -408,11 +435,9 @@ __global__ __launch_bounds__(kThreads, (ChunkCfg<D, BF16, MODE == kMoment || MOD
             for (int t = 0; t < NC; ++t) {
                 const int i = 16 * t + c16;
                 const uint32_t row = outr.off(i);
-                if (i < cnt)
-#pragma unroll
-                    for (int nb = 0; nb < NB; ++nb) {
-                        const v4f x = O[nb][t] * w.o_scale;
-                        const int col = mycol + 16 * nb + 4 * g4;
+                if (i < cnt) {
+                        const v4f x = O[t] * w.o_scale;
+                        const int col = mycol + 4 * g4;
                         if constexpr (MODE == kMoment) {
                             const char* p = outp + (row + col * ES);
                             v4f d;
@@ -427,21 +452,22 @@ __global__ __launch_bounds__(kThreads, (ChunkCfg<D, BF16, MODE == kMoment || MOD
                         } else {
                             char* p = const_cast<char*>(outp);
                             if (BF16 && !w.o_float) {
-                                const v4bf y = {(__bf16)x[0], (__bf16)x[1], (__bf16)x[2], (__bf16)x[3]};
+                                const v4bf y = __builtin_convertvector(x, v4bf);
                                 *reinterpret_cast<v4bf*>(p + (row + col * 2)) = y;
                             } else {
                                 *reinterpret_cast<v4f*>(p + (row + col * 4)) = x;
                             }
                         }
-                    }
+                }
             }
             if constexpr (MODE == kMoment) z += zc;
         }
 
+        // the next rows are on their way while S is updated, where registers are free for them
+        fetch(done + C);
+
         // S <- g^cnt S + K^T diag(g^(cnt-pre-j)) V, and T <- g^cnt (T + cnt S) + ... with the weights' derivative
         const float gc = expm1f(lg * (float)cnt);
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
             for (int j = 0; j < NJ; ++j)
 #pragma unroll
@@ -449,46 +475,39 @@ __global__ __launch_bounds__(kThreads, (ChunkCfg<D, BF16, MODE == kMoment || MOD
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         if constexpr (MOMENT) {
-                            const float x = fmaf((float)cnt, S[nb][j][a][i], T[nb][j][a][i]);
-                            T[nb][j][a][i] = fmaf(x, gc, x);
+                            const float x = fmaf((float)cnt, S[j][a][i], T[j][a][i]);
+                            T[j][a][i] = fmaf(x, gc, x);
                         }
-                        S[nb][j][a][i] = fmaf(S[nb][j][a][i], gc, S[nb][j][a][i]);
+                        S[j][a][i] = fmaf(S[j][a][i], gc, S[j][a][i]);
                     }
 #pragma unroll
         for (int kk = 0; kk < NK; ++kk) {
-            v8bf v[NB][3], m[MOMENT ? NB : 1][3];
-#pragma unroll
-            for (int nb = 0; nb < NB; ++nb) {
+            v8bf v[3], m[3];
                 v8bf raw[NT];
-                column(nb, kk, raw);
-                float x[8], y[8];
+                column(kk, raw);
+                v8f x = widen(raw[NT - 1]), y;
+#pragma unroll
+                for (int k = NT - 2; k >= 0; --k) x += widen(raw[k]);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    const int left = cnt - pre - (32 * kk + 8 * g4 + e);    // below 0 only for rows past the last, zero in LDS
-                    float f = (float)raw[NT - 1][e];
-#pragma unroll
-                    for (int k = NT - 2; k >= 0; --k) f += (float)raw[k][e];
-                    x[e] = f * pk[left < 0 ? 0 : left];
+                    const int left = cnt - pre - (32 * kk + 8 * g4 + e);
+                    x[e] *= pk[left];
                     if constexpr (MOMENT) y[e] = x[e] * (float)left;
                 }
-                split<3>(x, v[nb]);
-                if constexpr (MOMENT) split<3>(y, m[nb]);
-            }
+                split<3>(x, v);
+                if constexpr (MOMENT) split<3>(y, m);
 #pragma unroll
-            for (int j = 0; j < NJ; ++j)
+            for (int j = 0; j < NJ; ++j) {
+                v8bf kt[2][NT];
 #pragma unroll
-                for (int a = 0; a < 2; ++a) {
-                    v8bf kt[NT];
+                for (int a = 0; a < 2; ++a)
 #pragma unroll
                     for (int k = 0; k < NT; ++k)
-                        kt[k] = lds_turned(ki + (k * C + 32 * kk + 8 * g4 + (c16 >> 2)) * LD + 32 * j + 4 * a + 8 * (c16 & 3), 4 * LD);
-#pragma unroll
-                    for (int nb = 0; nb < NB; ++nb) {
-                        S[nb][j][a] = product<NT, 3>(kt, v[nb], S[nb][j][a]);
-                        if constexpr (MOMENT) T[nb][j][a] = product<NT, 3>(kt, m[nb], T[nb][j][a]);
-                    }
-                    if (a && (j & 1)) __builtin_amdgcn_sched_barrier(0);
-                }
+                        kt[a][k] = lds_turned(ki + (k * C + 32 * kk + 8 * g4 + (c16 >> 2)) * LD + 32 * j + 4 * a + 8 * (c16 & 3), 4 * LD);
+                products(kt, v, S[j]);
+                if constexpr (MOMENT) products(kt, m, T[j]);
+                if (j & 1) __builtin_amdgcn_sched_barrier(0);
+            }
             __builtin_amdgcn_sched_barrier(0);
         }
         __syncthreads();        // everybody is done with the images
@@ -497,7 +516,7 @@ __global__ __launch_bounds__(kThreads, (ChunkCfg<D, BF16, MODE == kMoment || MOD
     if constexpr (MODE == kOut) {
         // rows of this part that are not valid
         const int es = BF16 && !w.o_float ? 2 : 4, vecs = W * es / 16;
-        for (int i = tid; i < (rows - count) * vecs; i += kThreads) {
+        for (int i = tid; i < (rows - count) * vecs; i += THREADS) {
             char* p = row_of(w.o, b, row0 + count + i / vecs, h) + (size_t)col0 * es + i % vecs * 16;
             *reinterpret_cast<v4u*>(p) = v4u{0u, 0u, 0u, 0u};
         }
@@ -506,19 +525,17 @@ __global__ __launch_bounds__(kThreads, (ChunkCfg<D, BF16, MODE == kMoment || MOD
     if (STATES) to = w.parts + (((size_t)b * w.H + h) * (w.nparts - 1) + order) * D * D;
     else if (MODE != kMoment && order == w.nparts - 1 && w.state_out) to = w.state_out + state_at;
 #pragma unroll
-    for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
         for (int j = 0; j < NJ; ++j)
 #pragma unroll
             for (int a = 0; a < 2; ++a)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const size_t at = (size_t)(32 * j + 8 * g4 + 4 * a + i) * D + mycol + 16 * nb + c16;
-                    if (to) to[at] = S[nb][j][a][i];
+                    const size_t at = (size_t)(32 * j + 8 * g4 + 4 * a + i) * D + mycol + c16;
+                    if (to) to[at] = S[j][a][i];
                     if constexpr (MODE == kMomentState)
-                        w.part_moments[(((size_t)b * w.H + h) * (w.nparts - 1) + order) * D * D + at] = T[nb][j][a][i];
+                        w.part_moments[(((size_t)b * w.H + h) * (w.nparts - 1) + order) * D * D + at] = T[j][a][i];
                     if constexpr (MODE == kMoment)
-                        if (order == w.nparts - 1 && w.grad_state) z += (double)w.grad_state[state_at + at] * T[nb][j][a][i];
+                        if (order == w.nparts - 1 && w.grad_state) z += (double)w.grad_state[state_at + at] * T[j][a][i];
                 }
     if constexpr (MODE == kMoment) {
 #pragma unroll
@@ -527,16 +544,19 @@ __global__ __launch_bounds__(kThreads, (ChunkCfg<D, BF16, MODE == kMoment || MOD
         double* const sum = reinterpret_cast<double*>(lds);
         if (lane == 0) sum[wave] = z;
         __syncthreads();
-        if (tid == 0) w.moments[(((size_t)b * w.H + h) * w.nparts + part) * NS + slice] = sum[0] + sum[1] + sum[2] + sum[3];
+        if (tid == 0) {
+            for (int i = 1; i < NW; ++i) z += sum[i];
+            w.moments[(((size_t)b * w.H + h) * w.nparts + part) * NS + slice] = z;
+        }
     }
 }
 
 // parts[o] holds the state behind part o of the walk from a zero state; it becomes the state behind parts 0 .. o from
 // state_in, which is the start of part o + 1.
 template <bool MOMENT>
-__global__ __launch_bounds__(kThreads) void join_parts_kernel(Walk w) {
+__global__ __launch_bounds__(kJoinThreads) void join_parts_kernel(Walk w) {
     const int DD = w.D * w.D;
-    const size_t i = (size_t)blockIdx.x * kThreads + threadIdx.x;       // an element of a state
+    const size_t i = (size_t)blockIdx.x * kJoinThreads + threadIdx.x;   // an element of a state
     const int e = (int)(i % DD), h = (int)(i / DD % w.H), b = (int)(i / DD / w.H);
     const int len = user_len(w.lengths, b, w.N);
     const float lg = w.log_decay[h];
@@ -562,15 +582,15 @@ __global__ __launch_bounds__(kThreads) void join_parts_kernel(Walk w) {
 
 template <int D, bool BF16, int MODE>
 hipError_t launch(const Walk& w, int parts, hipStream_t stream) {
-    using F = ChunkCfg<D, BF16, MODE == kMoment || MODE == kMomentState>;
+    using F = ChunkCfg<D, BF16, is_moment(MODE)>;
     auto kern = decay_chunk_kernel<D, BF16, MODE>;
-    constexpr size_t bytes = F::lds_bytes(MODE == kOut || MODE == kMoment);
+    constexpr size_t bytes = F::lds_bytes(is_out(MODE));
     hipError_t e = allow_dynamic_lds(reinterpret_cast<const void*>(kern), bytes);
     if (e != hipSuccess) return e;
     const int share = w.k.share;
     const int64_t groups = (int64_t)w.B * w.H * parts / share;
     const int64_t blocks = (groups + 7) / 8 * 8 * share * (D / F::W);
-    hipLaunchKernelGGL(kern, dim3((unsigned)blocks), dim3(kThreads), bytes, stream, w);
+    hipLaunchKernelGGL(kern, dim3((unsigned)blocks), dim3(F::kThreads), bytes, stream, w);
     return hipGetLastError();
 }
 
@@ -580,9 +600,9 @@ hipError_t walk(const Walk& w, hipStream_t stream) {
     if (w.nparts > 1) {
         e = w.moment ? launch<D, BF16, kMomentState>(w, w.nparts - 1, stream) : launch<D, BF16, kState>(w, w.nparts - 1, stream);
         if (e != hipSuccess) return e;
-        const dim3 grid((unsigned)((size_t)w.B * w.H * D * D / kThreads));
-        if (w.moment) hipLaunchKernelGGL(join_parts_kernel<true>, grid, dim3(kThreads), 0, stream, w);
-        else hipLaunchKernelGGL(join_parts_kernel<false>, grid, dim3(kThreads), 0, stream, w);
+        const dim3 grid((unsigned)((size_t)w.B * w.H * D * D / kJoinThreads));
+        if (w.moment) hipLaunchKernelGGL(join_parts_kernel<true>, grid, dim3(kJoinThreads), 0, stream, w);
+        else hipLaunchKernelGGL(join_parts_kernel<false>, grid, dim3(kJoinThreads), 0, stream, w);
         e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
@@ -601,12 +621,12 @@ hipError_t launch_decay_chunks(const Walk& w, hipStream_t stream) {
     }
 }
 
-int moment_slices(int D) { return D / 64; }
+int moment_slices(int D) { return D < 128 ? 1 : D / 128; }
 
 // Parts that a sequence is cut into.  Two workgroups of the kernel fit a compute unit, so 512 fill the GPU; every part but
 // the last reads K and V once more, so there are no more than that takes, and none below eight chunks of 64 rows.
-DecayParts decay_parts(int B, int N, int H, int D, bool bf16) {
-    const int slices = bf16 && D == 128 ? 1 : D / 64;
+DecayParts decay_parts(int B, int N, int H, int D) {
+    const int slices = moment_slices(D);
     const int64_t have = (int64_t)B * H * slices;
     int64_t n = (512 + have - 1) / have;
     const int64_t most = N / 512;

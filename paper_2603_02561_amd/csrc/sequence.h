@@ -61,7 +61,7 @@ hipError_t launch_share_sum(const float* in, int B, int N, int H, int Hkv, int D
 struct DecayParts {
     int parts, rows;
 };
-DecayParts decay_parts(int B, int N, int H, int D, bool bf16);
+DecayParts decay_parts(int B, int N, int H, int D);
 int moment_slices(int D);
 hipError_t launch_decay_chunks(const Walk& w, hipStream_t stream);
 
