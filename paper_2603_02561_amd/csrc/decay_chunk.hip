@@ -29,9 +29,9 @@ struct ChunkCfg {
     static constexpr int kThreads = 4 * W;
     static constexpr int NT = BF16 ? 1 : 3;                             // terms of an input
     static constexpr int TP = BF16 && !MOMENT ? 2 : 3;                  // terms of P and S where they meet V and Q
-    static constexpr int LD = D + 8, LW = W + 8, LP = C + 8;            // bf16 per row of the images
-    static constexpr int kQ = NT * C * LD, kV = NT * C * LW, kP = TP * C * LP;
-    static constexpr size_t lds_bytes(bool out) { return 2 * (size_t)(kQ + kV + (out ? kQ + kP : 0)) + 4 * (3 * C + 2); }
+    static constexpr int LP = C + 8;                                    // bf16 per row of P's images
+    static constexpr int kQ = NT * C * D, kV = NT * C * W, kP = TP * C * LP;
+    static constexpr size_t lds_bytes(bool out) { return 2 * (size_t)(kQ + kV + (out ? kQ + kP : 0)) + 4 * (4 * C + 3 + 16); }
     // Waves per SIMD that the registers are shared out for: two workgroups per compute unit where LDS has room for two and
     // 128 registers hold what a wave needs.
     static constexpr int waves(bool out) { return 2 * lds_bytes(out) <= 160 * 1024 && !(D == 256 || (MOMENT && D == 128)) ? W / 32 : W / 64; }
@@ -100,15 +100,26 @@ __device__ __forceinline__ v4f product(const v8bf (&a)[TA], const v8bf (&b)[TB],
     return c;
 }
 
+// The images of rows in LDS have no padding: chunks of eight elements lie in row `row` at the place (chunk ^ swizzle(row)).  Then
+// neither the reads of one chunk from sixteen rows, nor the transposing reads of four rows, nor the stores of whole rows meet
+// in a bank (a row is 32, 64 or 128 of the 64 banks long).
+template <int COLS>
+__device__ __forceinline__ int swizzle(int row) {
+    if constexpr (COLS == 64) return ((row >> 1 & 1) << 2) | (row >> 2 & 3);
+    else return ((row & 3) << 2) | (row >> 2 & 3);
+}
+
 __device__ __forceinline__ v8bf lds8(const __bf16* p) { return *reinterpret_cast<const v8bf*>(p); }
 
-// Transposing read of 16-bit elements from rows r .. r+7 of an LDS image: lane i of a group of 16 passes the address of four
-// elements in row i/4 and receives element i%4 of the lanes i/4, 4 + i/4, 8 + i/4, 12 + i/4: rows 0..3 of "its" column.
-__device__ __forceinline__ v8bf lds_turned(const __bf16* p, int four_rows) {
+// Transposing read of 16-bit elements from eight rows r .. r+7, r a multiple of 8, of an image: lane i of a group of 16 passes
+// the address of four elements in row i/4 and receives element i%4 of the lanes i/4, 4 + i/4, 8 + i/4, 12 + i/4: rows 0..3 of
+// "its" column.  at: the place of its four elements in row r + i/4; four rows on a chunk lies at its place ^ 1.
+template <int COLS>
+__device__ __forceinline__ v8bf lds_turned(const __bf16* img, uint32_t at) {
     typedef short v4s __attribute__((ext_vector_type(4)));
     typedef __attribute__((address_space(3))) v4s* lds_ptr;
-    const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(p));
-    const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(p + four_rows));
+    const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(img + at));
+    const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(img + (at ^ 8) + 4 * COLS));
     typedef short v8s __attribute__((ext_vector_type(8)));
     const v8s r = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
     return __builtin_bit_cast(v8bf, r);
@@ -116,15 +127,18 @@ __device__ __forceinline__ v8bf lds_turned(const __bf16* p, int four_rows) {
 
 // Rows of one tensor, head and user in the order of the walk.  Addresses are a uniform base and a 32-bit offset per lane: row
 // i of the chunk that starts at row `done` is at(done) + off(i), at() lying below all rows of the chunk.
+template <int C>
 struct Rows {
     const char* first;
-    int64_t step;       // bytes; |step| * 64 < 2^31 by the host's checks
-    int64_t low;        // of the last row of a chunk where the walk goes down
+    int64_t step;           // bytes
+    uint32_t apart;         // |step| / 16, below 2^22 by the host's checks
+    uint32_t turn;          // C - 1 where the walk goes down, else 0
 
-    template <int C>
-    __device__ __forceinline__ static Rows make(const char* first, int64_t step) { return {first, step, step < 0 ? (C - 1) * step : 0}; }
-    __device__ __forceinline__ const char* at(int done) const { return first + done * step + low; }
-    __device__ __forceinline__ uint32_t off(int i) const { return (uint32_t)(i * (int)step - (int)low); }
+    __device__ __forceinline__ static Rows make(const char* first, int64_t step) {
+        return {first, step, (uint32_t)((step < 0 ? -step : step) / 16), step < 0 ? C - 1u : 0u};
+    }
+    __device__ __forceinline__ const char* at(int done) const { return first + done * step - (turn ? (int64_t)apart * 16 * (C - 1) : 0); }
+    __device__ __forceinline__ uint32_t off(uint32_t i) const { return __umul24(i ^ turn, apart) << 4; }
 };
 
 // One thread's share of the rows of a chunk on their way from memory to LDS: vectors of eight elements.
@@ -135,26 +149,27 @@ struct Fetch {
 
     // Row i is row done + i, or the last of the `count` rows where there are fewer: no branches, which would put the values
     // into scratch memory.
-    __device__ __forceinline__ void load(const Rows& r, int done, int count) {
+    __device__ __forceinline__ void load(const Rows<C>& r, int done, int count) {
         done = done < count ? done : count - 1;
         const char* p = r.at(done);
-        const int tid = fresh_tid(), i0 = tid / PER, c = tid % PER, last = count - 1 - done;
+        const uint32_t last = count - 1 - done, tid = fresh_tid(), i0 = tid / PER, col = tid % PER * (VS * 16);
 #pragma unroll
         for (int u = 0; u < N; ++u) {
-            const int i = i0 + u * (THREADS / PER);
-            const uint32_t off = r.off(i < last ? i : last) + c * VS * 16;
+            const uint32_t i = i0 + u * (THREADS / PER);
+            const uint32_t at = r.off(i < last ? i : last) + col;
 #pragma unroll
-            for (int v = 0; v < VS; ++v) x[u][v] = *reinterpret_cast<const v4u*>(p + (off + v * 16));
+            for (int v = 0; v < VS; ++v) x[u][v] = *reinterpret_cast<const v4u*>(p + (at + v * 16));
         }
     }
 
-    // to LDS, zeros for the rows from cnt on
-    __device__ __forceinline__ void store(__bf16* img, int ld, int cnt) const {
-        const int tid = fresh_tid();
+    __device__ __forceinline__ void store(__bf16* img) const {
+        const uint32_t tid = fresh_tid();
+        const int i0 = tid / PER, c = tid % PER;
+        // the rows of a thread are a multiple of 16 apart, so that its chunks have the same place in all of them
+        static_assert(N == 1 || THREADS / PER % 16 == 0, "");
+        __bf16* to = img + i0 * COLS + ((c ^ swizzle<COLS>(i0)) << 3);
 #pragma unroll
-        for (int u = 0; u < N; ++u) {
-            const int at = tid + u * THREADS, i = at / PER, c = at % PER;
-            __bf16* to = img + i * ld + 8 * c;
+        for (int u = 0; u < N; ++u, to += THREADS / PER * COLS) {
             if constexpr (BF16) {
                 *reinterpret_cast<v4u*>(to) = x[u][0];
             } else {
@@ -164,18 +179,18 @@ struct Fetch {
                 for (int e = 0; e < 8; ++e) f[e] = __uint_as_float(x[u][e / 4][e % 4]);
                 split<3>(f, s);
 #pragma unroll
-                for (int k = 0; k < 3; ++k) *reinterpret_cast<v8bf*>(to + k * C * ld) = s[k];
+                for (int k = 0; k < 3; ++k) *reinterpret_cast<v8bf*>(to + k * C * COLS) = s[k];
             }
         }
-        if (cnt < C) {
+    }
+
+    // the rows from cnt on
+    __device__ __forceinline__ static void clear(__bf16* img, int cnt) {
+#pragma unroll 1
+        for (int e = cnt * PER + threadIdx.x; e < C * PER; e += THREADS)
 #pragma unroll
-            for (int u = 0; u < N; ++u) {
-                const int at = tid + u * THREADS, i = at / PER, c = at % PER;
-                if (i >= cnt)
-#pragma unroll
-                    for (int k = 0; k < (BF16 ? 1 : 3); ++k) *reinterpret_cast<v4u*>(img + (k * C + i) * ld + 8 * c) = v4u{0u, 0u, 0u, 0u};
-            }
-        }
+            for (int k = 0; k < (BF16 ? 1 : 3); ++k)
+                *reinterpret_cast<v4u*>(img + k * C * COLS + (e << 3)) = v4u{0u, 0u, 0u, 0u};   // whole rows: no swizzle
     }
 };
 
@@ -191,15 +206,16 @@ __global__ __launch_bounds__((ChunkCfg<D, BF16, is_moment(MODE)>::kThreads), (Ch
 decay_chunk_kernel(Walk w) {
     constexpr bool MOMENT = is_moment(MODE), OUT = is_out(MODE), STATES = MODE == kState || MODE == kMomentState;
     using F = ChunkCfg<D, BF16, MOMENT>;
-    constexpr int C = F::C, W = F::W, THREADS = F::kThreads, NT = F::NT, TP = F::TP, LD = F::LD, LW = F::LW, LP = F::LP;
+    constexpr int C = F::C, W = F::W, THREADS = F::kThreads, NT = F::NT, TP = F::TP, LP = F::LP;
     constexpr int NW = THREADS / 64, NS = D / W, NJ = D / 32, NC = C / 16, NK = C / 32, ES = BF16 ? 2 : 4;
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    __bf16* const ki = reinterpret_cast<__bf16*>(lds);                  // [NT][C][LD]
-    __bf16* const vi = ki + F::kQ;                                      // [NT][C][LW]
-    __bf16* const qi = vi + F::kV;                                      // [NT][C][LD]
+    __bf16* const ki = reinterpret_cast<__bf16*>(lds);                  // [NT][C][D]
+    __bf16* const vi = ki + F::kQ;                                      // [NT][C][W]
+    __bf16* const qi = vi + F::kV;                                      // [NT][C][D]
     __bf16* const pi = qi + (OUT ? F::kQ : 0);                          // [TP][C][LP]: row t, column s
-    float* const pw = reinterpret_cast<float*>(pi + (OUT ? F::kP : 0)); // g^n, n = 0 .. C
+    float* const pw = reinterpret_cast<float*>(pi + (OUT ? F::kP : 0)); // o_scale g^n, n = 0 .. C
     float* const pk = pw + C + 1 + C;                                   // kv_scale g^n, n = -C .. C, zero below 0
+    float* const po = pk + C + 1 + 16;                                  // o_scale kv_scale g^n, n = -16 .. C, zero below 0
 
     // Slices of one part and heads that share K and V run on one XCD (workgroups go to the eight in turn), where they
     // find each other's rows in its L2.
@@ -211,8 +227,8 @@ decay_chunk_kernel(Walk w) {
     // in the order of the walk; the last part's state is nobody's start
     const int order = MODE == kLast ? w.nparts - 1 : (int)(unit / w.H % nparts), part = w.reverse ? w.nparts - 1 - order : order;
 
-    const int tid = threadIdx.x, lane = tid & 63;
-    int wave = tid >> 6, c16 = lane & 15, g4 = lane >> 4;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int c16 = lane & 15, g4 = lane >> 4;
     const int len = user_len(w.lengths, b, w.N);
     const int row0 = part * w.part_rows;                                // may not overflow: part < nparts
     const int rows = w.N - row0 < w.part_rows ? w.N - row0 : w.part_rows;
@@ -224,8 +240,10 @@ decay_chunk_kernel(Walk w) {
 
     for (int n = tid; n <= C; n += THREADS) {
         const float x = n ? expf(lg * (float)n) : 1.f;                  // log g may be -infinity
-        pw[n] = x;
+        pw[n] = w.o_scale * x;
         pk[n] = w.kv_scale * x;
+        po[n] = w.o_scale * w.kv_scale * x;
+        if (n && n <= 16) po[-n] = 0.f;
         if (n) pk[-n] = 0.f;
     }
 
@@ -258,12 +276,12 @@ decay_chunk_kernel(Walk w) {
 
     const int64_t step = w.reverse ? -1 : 1;
     const int64_t first = w.reverse ? row0 + (int64_t)count - 1 : row0;
-    const Rows kr = Rows::make<C>(row_of(w.k, b, first, h), step * w.k.s.row);
-    const Rows vr = Rows::make<C>(row_of(w.v, b, first, h) + (size_t)col0 * ES, step * w.v.s.row);
-    Rows qr = kr, outr = kr;                                            // of q, and of o or the gradient
-    if constexpr (OUT) qr = Rows::make<C>(row_of(w.q, b, first, h), step * w.q.s.row);
-    if constexpr (MODE == kOut) outr = Rows::make<C>(row_of(w.o, b, first, h), step * w.o.s.row);
-    if constexpr (MODE == kMoment) outr = Rows::make<C>(row_of(w.grad, b, first, h), step * w.grad.s.row);
+    const Rows<C> kr = Rows<C>::make(row_of(w.k, b, first, h), step * w.k.s.row);
+    const Rows<C> vr = Rows<C>::make(row_of(w.v, b, first, h) + (size_t)col0 * ES, step * w.v.s.row);
+    Rows<C> qr = kr, outr = kr;                                            // of q, and of o or the gradient
+    if constexpr (OUT) qr = Rows<C>::make(row_of(w.q, b, first, h), step * w.q.s.row);
+    if constexpr (MODE == kOut) outr = Rows<C>::make(row_of(w.o, b, first, h), step * w.o.s.row);
+    if constexpr (MODE == kMoment) outr = Rows<C>::make(row_of(w.grad, b, first, h), step * w.grad.s.row);
     Fetch<C, D, THREADS, BF16> fq, fk;
     Fetch<C, W, THREADS, BF16> fv;
     auto fetch = [&](int done) __attribute__((always_inline)) {
@@ -272,17 +290,28 @@ decay_chunk_kernel(Walk w) {
         if constexpr (OUT) fq.load(qr, done, count);
     };
     if (count) fetch(0);
+    // places in the images: chunk g4 of row c16; this lane's four elements of row 8 g4 + c16 / 4 for K^T (columns
+    // 8 (c16 % 4) ..) and for V (this wave's columns, 4 (c16 % 4) ..)
+    const int trow = 8 * g4 + (c16 >> 2);
+    uint32_t row_at = c16 * D + ((g4 ^ swizzle<D>(c16)) << 3), kt_at = trow * D + (((c16 & 3) ^ swizzle<D>(trow)) << 3),
+             v_at = trow * W + (((2 * wave + (c16 >> 1 & 1)) ^ swizzle<W>(trow)) << 3) + 4 * (c16 & 1);
+    const float gfull = expm1f(lg * (float)C);
     double z = 0.;          // terms of either sign over thousands of rows
 
     for (int done = 0; done < count; done += C) {
         const int cnt = count - done < C ? count - done : C;
-        {   // addresses are formed anew for every chunk, not kept in registers by the dozen
-            const int t = fresh_tid();
-            wave = t >> 6, c16 = t & 15, g4 = t >> 4 & 3;
+        // what follows from these is formed anew for every chunk, not kept in registers by the dozen
+        asm volatile("" : "+v"(row_at), "+v"(kt_at), "+v"(v_at));
+        const int ln = fresh_tid() & 63, c16 = ln & 15, g4 = ln >> 4;
+        fk.store(ki);
+        fv.store(vi);
+        if constexpr (OUT) fq.store(qi);
+        if (cnt < C) {
+            __syncthreads();
+            fk.clear(ki, cnt);
+            fv.clear(vi, cnt);
+            if constexpr (OUT) fq.clear(qi, cnt);
         }
-        fk.store(ki, LD, cnt);
-        fv.store(vi, LW, cnt);
-        if constexpr (OUT) fq.store(qi, LD, cnt);
         __syncthreads();
 
         v4f O[NC];
@@ -310,7 +339,7 @@ decay_chunk_kernel(Walk w) {
 #pragma unroll
                 for (int t = 0; t < NC; ++t)
 #pragma unroll
-                    for (int k = 0; k < NT; ++k) q[t][k] = lds8(qi + (k * C + 16 * t + c16) * LD + 32 * j + 8 * g4);
+                    for (int k = 0; k < NT; ++k) q[t][k] = lds8(qi + (k * C + 16 * t) * D + (row_at ^ j << 5));
                 products(s, q, O);
                 if constexpr (MOMENT) products(m, q, R);
                 // or the operands of all steps are read at once, and registers spilled
@@ -334,15 +363,15 @@ decay_chunk_kernel(Walk w) {
                     v8bf a[NT], q[NT];
 #pragma unroll
                     for (int k = 0; k < NT; ++k) {
-                        a[k] = lds8(ki + (k * C + 16 * sb + c16) * LD + 32 * j + 8 * g4);
-                        q[k] = lds8(qi + (k * C + 16 * tb + c16) * LD + 32 * j + 8 * g4);
+                        a[k] = lds8(ki + (k * C + 16 * sb) * D + (row_at ^ j << 5));
+                        q[k] = lds8(qi + (k * C + 16 * tb) * D + (row_at ^ j << 5));
                     }
                     p = product<NT, NT>(a, q, p);
                 }
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const int ago = 16 * (tb - sb) + c16 - 4 * g4 - i;
-                    const float wgt = MOMENT ? pk[ago] * (float)ago : pk[ago];
+                    const float wgt = MOMENT ? po[ago] * (float)ago : po[ago];
                     p[i] = ago < 0 ? 0.f : p[i] * wgt;          // not 0 * p: rows after t may hold anything
                 }
 #pragma unroll
@@ -368,7 +397,7 @@ decay_chunk_kernel(Walk w) {
         auto column = [&](int kk, v8bf (&v)[NT]) __attribute__((always_inline)) {
 #pragma unroll
             for (int k = 0; k < NT; ++k)
-                v[k] = lds_turned(vi + (k * C + 32 * kk + 8 * g4 + (c16 >> 2)) * LW + wave * 16 + 4 * (c16 & 3), 4 * LW);
+                v[k] = lds_turned<W>(vi + (k * C + 32 * kk) * W, v_at);
         };
         if constexpr (OUT) {
 #pragma unroll
@@ -391,11 +420,10 @@ decay_chunk_kernel(Walk w) {
             }
             // A row of V that is not finite reaches the rows before it here, as 0 * V.  Then the products are taken again with
             // zeros for such values, and a column that has met one by row t is NaN from there on: the same products count them.
+            // The last tile meets all rows of V.
             float probe = 0.f;
 #pragma unroll
-                for (int t = 0; t < NC; ++t)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) probe = fmaf(O[t][i], 0.f, probe);
+            for (int i = 0; i < 4; ++i) probe = fmaf(O[NC - 1][i], 0.f, probe);
             __builtin_amdgcn_sched_barrier(0);
             if (__builtin_expect(__any(probe != 0.f), 0)) {
                 from_state();
@@ -434,30 +462,24 @@ decay_chunk_kernel(Walk w) {
 #pragma unroll
             for (int t = 0; t < NC; ++t) {
                 const int i = 16 * t + c16;
-                const uint32_t row = outr.off(i);
+                const uint32_t at = outr.off(i) + (mycol + 4 * g4) * (BF16 && !(MODE == kOut && w.o_float) ? 2 : 4);
                 if (i < cnt) {
-                        const v4f x = O[t] * w.o_scale;
-                        const int col = mycol + 4 * g4;
-                        if constexpr (MODE == kMoment) {
-                            const char* p = outp + (row + col * ES);
-                            v4f d;
-                            if constexpr (BF16) {
-                                const uint2 u = *reinterpret_cast<const uint2*>(p);
-                                d = v4f{bf16_lo(u.x), bf16_hi(u.x), bf16_lo(u.y), bf16_hi(u.y)};
-                            } else {
-                                d = *reinterpret_cast<const v4f*>(p);
-                            }
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) zc = fmaf(x[e], d[e], zc);
+                    const v4f x = O[t];
+                    if constexpr (MODE == kMoment) {
+                        v4f d;
+                        if constexpr (BF16) {
+                            const uint2 u = *reinterpret_cast<const uint2*>(outp + at);
+                            d = v4f{bf16_lo(u.x), bf16_hi(u.x), bf16_lo(u.y), bf16_hi(u.y)};
                         } else {
-                            char* p = const_cast<char*>(outp);
-                            if (BF16 && !w.o_float) {
-                                const v4bf y = __builtin_convertvector(x, v4bf);
-                                *reinterpret_cast<v4bf*>(p + (row + col * 2)) = y;
-                            } else {
-                                *reinterpret_cast<v4f*>(p + (row + col * 4)) = x;
-                            }
+                            d = *reinterpret_cast<const v4f*>(outp + at);
                         }
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) zc = fmaf(x[e], d[e], zc);
+                    } else {
+                        char* p = const_cast<char*>(outp + at);
+                        if (BF16 && !w.o_float) *reinterpret_cast<v4bf*>(p) = __builtin_convertvector(x, v4bf);
+                        else *reinterpret_cast<v4f*>(p) = x;
+                    }
                 }
             }
             if constexpr (MODE == kMoment) z += zc;
@@ -467,7 +489,7 @@ decay_chunk_kernel(Walk w) {
         fetch(done + C);
 
         // S <- g^cnt S + K^T diag(g^(cnt-pre-j)) V, and T <- g^cnt (T + cnt S) + ... with the weights' derivative
-        const float gc = expm1f(lg * (float)cnt);
+        const float gc = cnt == C ? gfull : expm1f(lg * (float)cnt);
 #pragma unroll
             for (int j = 0; j < NJ; ++j)
 #pragma unroll
@@ -503,7 +525,7 @@ decay_chunk_kernel(Walk w) {
                 for (int a = 0; a < 2; ++a)
 #pragma unroll
                     for (int k = 0; k < NT; ++k)
-                        kt[a][k] = lds_turned(ki + (k * C + 32 * kk + 8 * g4 + (c16 >> 2)) * LD + 32 * j + 4 * a + 8 * (c16 & 3), 4 * LD);
+                        kt[a][k] = lds_turned<D>(ki + (k * C + 32 * kk) * D + 4 * a, kt_at ^ j << 5);
                 products(kt, v, S[j]);
                 if constexpr (MOMENT) products(kt, m, T[j]);
                 if (j & 1) __builtin_amdgcn_sched_barrier(0);
