@@ -247,8 +247,19 @@ solar_status solar_decay_attention_backward(const void* Q, const void* K, const 
     a.in_turned = true;
     a.o_scale = scale;
     a.kv_scale = 1.f;
+    if (dlog_decay) {
+        // sum_t <do_t, d o_t / d log g>: o_t = scale S_t^T q_t, so the same walk gives it as <q_t, d dq_t / d log g>
+        a.moment = true;
+        a.grad = q;
+        a.grad_state = dstate_out;
+        a.moments = c.moments;
+    }
     hipError_t e = launch_decay_chunks(a, st);
     if (e != hipSuccess) return SOLAR_ERR_HIP;
+    if (dlog_decay) {
+        e = launch_moment_sum(c.moments, B, H, c.cut.parts * moment_slices(D), dlog_decay, st);
+        if (e != hipSuccess) return SOLAR_ERR_HIP;
+    }
     // dv_t = G_t^T k_t, dk_t = G_t v_t with G_t = scale q_t do_t^T + g G_{t+1}: walks from the last row on
     Walk d = w;
     d.reverse = true;
@@ -272,22 +283,6 @@ solar_status solar_decay_attention_backward(const void* Q, const void* K, const 
         e = launch_share_sum(c.dk, B, N, H, Hkv, D, dk, w.bf16, st);
         if (e != hipSuccess) return SOLAR_ERR_HIP;
         e = launch_share_sum(c.dv, B, N, H, Hkv, D, dv, w.bf16, st);
-        if (e != hipSuccess) return SOLAR_ERR_HIP;
-    }
-    if (dlog_decay) {
-        // sum_t do_t . o'_t with o' the derivative of the outputs by log g: its state T_t = g (T_{t-1} + S_{t-1})
-        Walk m = w;
-        m.q = q; m.k = k; m.v = vv;
-        m.state_in = state_in;
-        m.o_scale = scale;
-        m.kv_scale = 1.f;
-        m.moment = true;
-        m.grad = g;
-        m.grad_state = dstate_out;
-        m.moments = c.moments;
-        e = launch_decay_chunks(m, st);
-        if (e != hipSuccess) return SOLAR_ERR_HIP;
-        e = launch_moment_sum(c.moments, B, H, c.cut.parts * moment_slices(D), dlog_decay, st);
         if (e != hipSuccess) return SOLAR_ERR_HIP;
     }
     return SOLAR_OK;

@@ -24,17 +24,20 @@ typedef __bf16 v4bf __attribute__((ext_vector_type(4)));
 
 template <int D, bool BF16, bool MOMENT>
 struct ChunkCfg {
-    static constexpr int C = BF16 && D <= 128 && !MOMENT ? 64 : 32;     // rows of a chunk
-    static constexpr int W = D < 128 ? D : 128;                         // columns of S per workgroup, 16 per wave
-    static constexpr int kThreads = 4 * W;
+    static constexpr int C = BF16 && D <= 128 ? 64 : 32;                // rows of a chunk
+    static constexpr int W = D == 64 || (MOMENT && D == 256) ? 64 : 128;    // columns of S per workgroup
+    // Tiles of 16 columns per wave.  Every wave reads all of Q and K from LDS, so two tiles halve that: at D = 128 the registers
+    // of two waves per SIMD hold them.
+    static constexpr int NB = D == 128 && !MOMENT ? 2 : 1;
+    static constexpr int kThreads = 4 * W / NB;
     static constexpr int NT = BF16 ? 1 : 3;                             // terms of an input
-    static constexpr int TP = BF16 && !MOMENT ? 2 : 3;                  // terms of P and S where they meet V and Q
+    static constexpr int TP = BF16 ? 2 : 3;                             // terms of P and S where they meet V and Q
     static constexpr int LP = C + 8;                                    // bf16 per row of P's images
-    static constexpr int kQ = NT * C * D, kV = NT * C * W, kP = TP * C * LP;
-    static constexpr size_t lds_bytes(bool out) { return 2 * (size_t)(kQ + kV + (out ? kQ + kP : 0)) + 4 * (4 * C + 3 + 16); }
-    // Waves per SIMD that the registers are shared out for: two workgroups per compute unit where LDS has room for two and
-    // 128 registers hold what a wave needs.
-    static constexpr int waves(bool out) { return 2 * lds_bytes(out) <= 160 * 1024 && !(D == 256 || (MOMENT && D == 128)) ? W / 32 : W / 64; }
+    static constexpr int kQ = NT * C * D, kV = NT * C * W, kP = (TP + (MOMENT ? 3 : 0)) * C * LP;
+    static constexpr int kTables = 4 * C + 3 + 16;
+    static constexpr size_t lds_bytes(bool out) { return 2 * (size_t)(kQ + kV + (out ? kQ + kP : 0)) + 4 * kTables; }
+    // waves per SIMD that the registers are shared out for
+    static constexpr int waves(bool out) { return MOMENT ? 2 : out ? (D == 64 ? 3 : 2) : (D == 128 ? 3 : 4); }
 };
 
 typedef float v8f __attribute__((ext_vector_type(8)));
@@ -63,10 +66,10 @@ __device__ __forceinline__ void split(v8f x, v8bf (&s)[T]) {
 
 __device__ __forceinline__ v4f mfma(v8bf a, v8bf b, v4f c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 
-// c[n] + a[n] b[n] over the pairs of terms that matter, the small ones first; the products that follow one another are
-// independent.  a or b is the same for all n.
-template <int N, int TA, int TB>
-__device__ __forceinline__ void products(const v8bf (&a)[TA], const v8bf (&b)[N][TB], v4f (&c)[N]) {
+// c[m][n] + a[m] b[n] over the pairs of terms that matter, the small ones first; products that follow one another are
+// independent.
+template <int M, int N, int TA, int TB>
+__device__ __forceinline__ void products(const v8bf (&a)[M][TA], const v8bf (&b)[N][TB], v4f (&c)[M][N]) {
     constexpr int T = TA > TB ? TA : TB;
 #pragma unroll
     for (int sum = T - 1; sum >= 0; --sum)
@@ -74,30 +77,9 @@ __device__ __forceinline__ void products(const v8bf (&a)[TA], const v8bf (&b)[N]
         for (int i = 0; i < TA; ++i)
             if (sum - i >= 0 && sum - i < TB)
 #pragma unroll
-                for (int n = 0; n < N; ++n) c[n] = mfma(a[i], b[n][sum - i], c[n]);
-}
-
-template <int N, int TA, int TB>
-__device__ __forceinline__ void products(const v8bf (&a)[N][TA], const v8bf (&b)[TB], v4f (&c)[N]) {
-    constexpr int T = TA > TB ? TA : TB;
+                for (int m = 0; m < M; ++m)
 #pragma unroll
-    for (int sum = T - 1; sum >= 0; --sum)
-#pragma unroll
-        for (int i = 0; i < TA; ++i)
-            if (sum - i >= 0 && sum - i < TB)
-#pragma unroll
-                for (int n = 0; n < N; ++n) c[n] = mfma(a[n][i], b[sum - i], c[n]);
-}
-
-template <int TA, int TB>
-__device__ __forceinline__ v4f product(const v8bf (&a)[TA], const v8bf (&b)[TB], v4f c) {
-    constexpr int T = TA > TB ? TA : TB;
-#pragma unroll
-    for (int sum = T - 1; sum >= 0; --sum)
-#pragma unroll
-        for (int i = 0; i < TA; ++i)
-            if (sum - i >= 0 && sum - i < TB) c = mfma(a[i], b[sum - i], c);
-    return c;
+                    for (int n = 0; n < N; ++n) c[m][n] = mfma(a[m][i], b[n][sum - i], c[m][n]);
 }
 
 // The images of rows in LDS have no padding: chunks of eight elements lie in row `row` at the place (chunk ^ swizzle(row)).  Then
@@ -165,11 +147,12 @@ struct Fetch {
     __device__ __forceinline__ void store(__bf16* img) const {
         const uint32_t tid = fresh_tid();
         const int i0 = tid / PER, c = tid % PER;
-        // the rows of a thread are a multiple of 16 apart, so that its chunks have the same place in all of them
-        static_assert(N == 1 || THREADS / PER % 16 == 0, "");
-        __bf16* to = img + i0 * COLS + ((c ^ swizzle<COLS>(i0)) << 3);
+        constexpr int APART = THREADS / PER;        // rows; their chunks have one place in all of them where it is a multiple of 16
+        const int place = (c ^ swizzle<COLS>(i0)) << 3;
 #pragma unroll
-        for (int u = 0; u < N; ++u, to += THREADS / PER * COLS) {
+        for (int u = 0; u < N; ++u) {
+            const int i = i0 + u * APART;
+            __bf16* to = img + i * COLS + (APART % 16 ? (c ^ swizzle<COLS>(i)) << 3 : place);
             if constexpr (BF16) {
                 *reinterpret_cast<v4u*>(to) = x[u][0];
             } else {
@@ -194,9 +177,29 @@ struct Fetch {
     }
 };
 
-// kOut: outputs; kState: the state behind each part but the last, from a zero state, into w.parts; kMoment: the derivative of
-// the outputs by log g, summed against their gradient; kMomentState: kState, and the derivative of these states; kLast: the
-// state behind the last part, where nobody wants outputs.
+template <int K>
+struct Terms {
+    static constexpr int value = K;
+};
+
+// c[nb][a] + k[a] v[nb]: the same with the roles of rows and columns of c exchanged
+template <int A, int NB, int TA, int TB>
+__device__ __forceinline__ void update(const v8bf (&k)[A][TA], const v8bf (&v)[NB][TB], v4f (&c)[NB][A]) {
+    constexpr int T = TA > TB ? TA : TB;
+#pragma unroll
+    for (int sum = T - 1; sum >= 0; --sum)
+#pragma unroll
+        for (int i = 0; i < TA; ++i)
+            if (sum - i >= 0 && sum - i < TB)
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                    for (int a = 0; a < A; ++a) c[nb][a] = mfma(k[a][i], v[nb][sum - i], c[nb][a]);
+}
+
+// kOut: outputs; kState: the state behind each part but the last, from a zero state, into w.parts; kMoment: outputs, and their
+// derivative by log g summed against w.grad; kMomentState: kState, and the derivative of these states; kLast: the state behind
+// the last part, where nobody wants outputs.
 enum { kOut, kState, kMoment, kMomentState, kLast };
 constexpr bool is_moment(int mode) { return mode == kMoment || mode == kMomentState; }
 constexpr bool is_out(int mode) { return mode == kOut || mode == kMoment; }
@@ -206,13 +209,15 @@ __global__ __launch_bounds__((ChunkCfg<D, BF16, is_moment(MODE)>::kThreads), (Ch
 decay_chunk_kernel(Walk w) {
     constexpr bool MOMENT = is_moment(MODE), OUT = is_out(MODE), STATES = MODE == kState || MODE == kMomentState;
     using F = ChunkCfg<D, BF16, MOMENT>;
-    constexpr int C = F::C, W = F::W, THREADS = F::kThreads, NT = F::NT, TP = F::TP, LP = F::LP;
+    constexpr int C = F::C, W = F::W, NB = F::NB, THREADS = F::kThreads, NT = F::NT, TP = F::TP, LP = F::LP;
     constexpr int NW = THREADS / 64, NS = D / W, NJ = D / 32, NC = C / 16, NK = C / 32, ES = BF16 ? 2 : 4;
+    constexpr int TM = MOMENT ? 3 : 1, MB = MOMENT ? NB : 1, MJ = MOMENT ? NJ : 1;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     __bf16* const ki = reinterpret_cast<__bf16*>(lds);                  // [NT][C][D]
     __bf16* const vi = ki + F::kQ;                                      // [NT][C][W]
     __bf16* const qi = vi + F::kV;                                      // [NT][C][D]
     __bf16* const pi = qi + (OUT ? F::kQ : 0);                          // [TP][C][LP]: row t, column s
+    __bf16* const mi = pi + TP * C * LP;                                // [3][C][LP] with MOMENT: the same, times t - s
     float* const pw = reinterpret_cast<float*>(pi + (OUT ? F::kP : 0)); // o_scale g^n, n = 0 .. C
     float* const pk = pw + C + 1 + C;                                   // kv_scale g^n, n = -C .. C, zero below 0
     float* const po = pk + C + 1 + 16;                                  // o_scale kv_scale g^n, n = -16 .. C, zero below 0
@@ -227,61 +232,71 @@ decay_chunk_kernel(Walk w) {
     // in the order of the walk; the last part's state is nobody's start
     const int order = MODE == kLast ? w.nparts - 1 : (int)(unit / w.H % nparts), part = w.reverse ? w.nparts - 1 - order : order;
 
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int c16 = lane & 15, g4 = lane >> 4;
+    const int tid = threadIdx.x, wave = tid >> 6;
     const int len = user_len(w.lengths, b, w.N);
-    const int row0 = part * w.part_rows;                                // may not overflow: part < nparts
+    const int row0 = part * w.part_rows;
     const int rows = w.N - row0 < w.part_rows ? w.N - row0 : w.part_rows;
     const int count = len - row0 < 0 ? 0 : (len - row0 < rows ? len - row0 : rows);
     const int pre = w.reverse ? 0 : 1;
     const float lg = w.log_decay[h];
-    const int col0 = slice * W;                                         // this workgroup's columns of S
-    const int mycol = col0 + wave * 16;                            // this wave's
+    const int col0 = slice * W, mycol = col0 + wave * 16 * NB;          // the workgroup's columns of S, and the wave's
 
     for (int n = tid; n <= C; n += THREADS) {
         const float x = n ? expf(lg * (float)n) : 1.f;                  // log g may be -infinity
         pw[n] = w.o_scale * x;
         pk[n] = w.kv_scale * x;
         po[n] = w.o_scale * w.kv_scale * x;
-        if (n && n <= 16) po[-n] = 0.f;
         if (n) pk[-n] = 0.f;
+        if (n && n <= 16) po[-n] = 0.f;
     }
-
     if constexpr (OUT) {
         // P above the diagonal, as far as the 32 rows of V that a product takes reach: zero, and never written again
-        for (int n = tid; n < TP * C * 2; n += THREADS) {
+        for (int n = tid; n < F::kP / LP * 2; n += THREADS) {
             const int t = n / 2 % C, k = n / 2 / C;
             if (!(t & 16)) *reinterpret_cast<v4u*>(pi + (k * C + t) * LP + (t & ~15) + 16 + 8 * (n & 1)) = v4u{0u, 0u, 0u, 0u};
         }
     }
 
-    // S[j][a]: rows 32 j + 8 g4 + 4 a + (0..3), column mycol + c16
-    v4f S[NJ][2], T[MOMENT ? NJ : 1][2];
+    // S[j][nb][a]: rows 32 j + 8 g4 + 4 a + (0..3), column mycol + 16 nb + c16 for lane 16 g4 + c16; T: its derivative
+    v4f S[NJ][NB][2], T[MJ][MB][2];
     const size_t state_at = ((size_t)b * w.H + h) * D * D;
-    const size_t part_at = (((size_t)b * w.H + h) * (w.nparts - 1) + (order - 1)) * D * D;   // order > 0 only
-    const float* start = w.nparts == 1 || order == 0 ? (w.state_in ? w.state_in + state_at : nullptr) : w.parts + part_at;
-    const bool turned = order == 0 && w.in_turned;
-    if (STATES) start = nullptr;
+    const size_t part_at = ((size_t)b * w.H + h) * (w.nparts - 1) * D * D;
+    // f(the place of an entry in a state, the same in a transposed one, j, nb, a, i)
+    auto entries = [&](auto f) __attribute__((always_inline)) {
+        const int c16 = tid & 15, g4 = tid >> 4 & 3;
 #pragma unroll
         for (int j = 0; j < NJ; ++j)
 #pragma unroll
-            for (int a = 0; a < 2; ++a)
+            for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int r = 32 * j + 8 * g4 + 4 * a + i, col = mycol + c16;
-                    S[j][a][i] = start ? start[turned ? (size_t)col * D + r : (size_t)r * D + col] : 0.f;
-                    if constexpr (MOMENT)
-                        T[j][a][i] = MODE == kMoment && order > 0 ? w.part_moments[part_at + (size_t)r * D + col] : 0.f;
-                }
+                for (int a = 0; a < 2; ++a)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int r = 32 * j + 8 * g4 + 4 * a + i, col = mycol + 16 * nb + c16;
+                        f((uint32_t)(r * D + col), (uint32_t)(col * D + r), j, nb, a, i);
+                    }
+    };
+    {
+        const bool own = order > 0 && !STATES;          // starts where the part before ends
+        const float* start = STATES ? nullptr : own ? w.parts + part_at + (size_t)(order - 1) * D * D
+                                                    : w.state_in ? w.state_in + state_at : nullptr;
+        const bool turned = !own && w.in_turned;
+        entries([&](uint32_t at, uint32_t across, int j, int nb, int a, int i) {
+            S[j][nb][a][i] = start ? start[turned ? across : at] : 0.f;
+            if constexpr (MOMENT) T[j][nb][a][i] = own ? w.part_moments[part_at + (size_t)(order - 1) * D * D + at] : 0.f;
+        });
+    }
 
     const int64_t step = w.reverse ? -1 : 1;
     const int64_t first = w.reverse ? row0 + (int64_t)count - 1 : row0;
     const Rows<C> kr = Rows<C>::make(row_of(w.k, b, first, h), step * w.k.s.row);
     const Rows<C> vr = Rows<C>::make(row_of(w.v, b, first, h) + (size_t)col0 * ES, step * w.v.s.row);
-    Rows<C> qr = kr, outr = kr;                                            // of q, and of o or the gradient
-    if constexpr (OUT) qr = Rows<C>::make(row_of(w.q, b, first, h), step * w.q.s.row);
-    if constexpr (MODE == kOut) outr = Rows<C>::make(row_of(w.o, b, first, h), step * w.o.s.row);
-    if constexpr (MODE == kMoment) outr = Rows<C>::make(row_of(w.grad, b, first, h), step * w.grad.s.row);
+    Rows<C> qr = kr, outr = kr, gradr = kr;
+    if constexpr (OUT) {
+        qr = Rows<C>::make(row_of(w.q, b, first, h), step * w.q.s.row);
+        outr = Rows<C>::make(row_of(w.o, b, first, h), step * w.o.s.row);
+    }
+    if constexpr (MODE == kMoment) gradr = Rows<C>::make(row_of(w.grad, b, first, h), step * w.grad.s.row);
     Fetch<C, D, THREADS, BF16> fq, fk;
     Fetch<C, W, THREADS, BF16> fv;
     auto fetch = [&](int done) __attribute__((always_inline)) {
@@ -290,11 +305,16 @@ decay_chunk_kernel(Walk w) {
         if constexpr (OUT) fq.load(qr, done, count);
     };
     if (count) fetch(0);
+
     // places in the images: chunk g4 of row c16; this lane's four elements of row 8 g4 + c16 / 4 for K^T (columns
     // 8 (c16 % 4) ..) and for V (this wave's columns, 4 (c16 % 4) ..)
-    const int trow = 8 * g4 + (c16 >> 2);
-    uint32_t row_at = c16 * D + ((g4 ^ swizzle<D>(c16)) << 3), kt_at = trow * D + (((c16 & 3) ^ swizzle<D>(trow)) << 3),
-             v_at = trow * W + (((2 * wave + (c16 >> 1 & 1)) ^ swizzle<W>(trow)) << 3) + 4 * (c16 & 1);
+    uint32_t row_at, kt_at, v_at;
+    {
+        const int c16 = tid & 15, g4 = tid >> 4 & 3, trow = 8 * g4 + (c16 >> 2);
+        row_at = c16 * D + ((g4 ^ swizzle<D>(c16)) << 3);
+        kt_at = trow * D + (((c16 & 3) ^ swizzle<D>(trow)) << 3);
+        v_at = trow * W + (((2 * NB * wave + (c16 >> 1 & 1)) ^ swizzle<W>(trow)) << 3) + 4 * (c16 & 1);
+    }
     const float gfull = expm1f(lg * (float)C);
     double z = 0.;          // terms of either sign over thousands of rows
 
@@ -314,174 +334,251 @@ decay_chunk_kernel(Walk w) {
         }
         __syncthreads();
 
-        v4f O[NC];
-        // Q S, times g^(i+pre)
+        // V's rows 32 kk + 8 g4 + (0..7) of this wave's columns
+        auto read_v = [&](int kk, v8bf (&v)[NB][NT]) __attribute__((always_inline)) {
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                for (int k = 0; k < NT; ++k) v[nb][k] = lds_turned<W>(vi + (k * C + 32 * kk) * W, v_at ^ (nb << 4));
+        };
+        v4f O[NB][NC], R[MB][MOMENT ? NC : 1];
+        // O = Q S times g^(i+pre), R its derivative
         auto from_state = [&]() __attribute__((always_inline)) {
 #pragma unroll
-                for (int t = 0; t < NC; ++t) O[t] = v4f{0.f, 0.f, 0.f, 0.f};
-            v4f R[NC];
-            if constexpr (MOMENT)
+            for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-                    for (int t = 0; t < NC; ++t) R[t] = v4f{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int j = 0; j < NJ; ++j) {
-                v8bf s[TP], m[TP];
-                    v8f x;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) x[e] = S[j][e / 4][e % 4];
-                    split<TP>(x, s);
-                    if constexpr (MOMENT) {
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) x[e] = T[j][e / 4][e % 4];
-                        split<TP>(x, m);
-                    }
-                v8bf q[NC][NT];
+                for (int t = 0; t < NC; ++t) {
+                    O[nb][t] = v4f{0.f, 0.f, 0.f, 0.f};
+                    if constexpr (MOMENT) R[nb][t] = v4f{0.f, 0.f, 0.f, 0.f};
+                }
+            v8bf q[2][NC][NT];
+            auto read_q = [&](int j) __attribute__((always_inline)) {
 #pragma unroll
                 for (int t = 0; t < NC; ++t)
 #pragma unroll
-                    for (int k = 0; k < NT; ++k) q[t][k] = lds8(qi + (k * C + 16 * t) * D + (row_at ^ j << 5));
-                products(s, q, O);
-                if constexpr (MOMENT) products(m, q, R);
+                    for (int k = 0; k < NT; ++k) q[j & 1][t][k] = lds8(qi + (k * C + 16 * t) * D + (row_at ^ (j << 5)));
+            };
+            read_q(0);
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) {
+                if (j + 1 < NJ) read_q(j + 1);
+                v8bf s[NB][TP];
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) {
+                    v8f x;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) x[e] = S[j][nb][e / 4][e % 4];
+                    split<TP>(x, s[nb]);
+                }
+                products(s, q[j & 1], O);
+                if constexpr (MOMENT) {
+                    v8bf m[NB][3];
+#pragma unroll
+                    for (int nb = 0; nb < NB; ++nb) {
+                        v8f x;
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) x[e] = T[j][nb][e / 4][e % 4];
+                        split<3>(x, m[nb]);
+                    }
+                    products(m, q[j & 1], R);
+                }
                 // or the operands of all steps are read at once, and registers spilled
                 __builtin_amdgcn_sched_barrier(0);
             }
 #pragma unroll
             for (int t = 0; t < NC; ++t) {
-                const int i = 16 * t + c16;
-                const float x = pw[i + pre];
-                    if constexpr (MOMENT) O[t] = (R[t] + (float)(i + 1) * O[t]) * x;
-                    else O[t] *= x;
+                const float x = pw[16 * t + c16 + pre];
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) {
+                    if constexpr (MOMENT) R[nb][t] = (R[nb][t] + (float)(16 * t + c16 + pre) * O[nb][t]) * x;
+                    O[nb][t] *= x;
+                }
             }
         };
 
         if constexpr (OUT) {
-            // P^T, rows s, columns t, in tiles of 16: those up to the diagonal go round the waves
-            auto tile = [&](int sb, int tb) __attribute__((always_inline)) {
-                v4f p = {0.f, 0.f, 0.f, 0.f};
+            // P^T, rows s, columns t, in tiles of 16: those up to the diagonal go round the waves, and every wave takes all of
+            // its tiles at once (the last one twice where they do not come out even)
+            constexpr int TILES = NC * (NC + 1) / 2, MINE = (TILES + NW - 1) / NW;
+            int sb[MINE], tb[MINE];
+            v4f p[MINE];
 #pragma unroll
-                for (int j = 0; j < NJ; ++j) {
-                    v8bf a[NT], q[NT];
+            for (int y = 0; y < MINE; ++y) {
+                const int n = wave + y * NW < TILES ? wave + y * NW : TILES - 1;
+                tb[y] = __builtin_amdgcn_readfirstlane(n < 1 ? 0 : n < 3 ? 1 : n < 6 ? 2 : 3);
+                sb[y] = __builtin_amdgcn_readfirstlane(n) - tb[y] * (tb[y] + 1) / 2;
+                p[y] = v4f{0.f, 0.f, 0.f, 0.f};
+            }
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) {
+#pragma unroll
+                for (int y = 0; y < MINE; ++y) {
+                    v8bf a[1][NT], q[1][NT];
 #pragma unroll
                     for (int k = 0; k < NT; ++k) {
-                        a[k] = lds8(ki + (k * C + 16 * sb) * D + (row_at ^ j << 5));
-                        q[k] = lds8(qi + (k * C + 16 * tb) * D + (row_at ^ j << 5));
+                        a[0][k] = lds8(ki + (k * C + 16 * sb[y]) * D + (row_at ^ (j << 5)));
+                        q[0][k] = lds8(qi + (k * C + 16 * tb[y]) * D + (row_at ^ (j << 5)));
                     }
-                    p = product<NT, NT>(a, q, p);
+                    v4f c[1][1] = {{p[y]}};
+                    products(a, q, c);
+                    p[y] = c[0][0];
                 }
+                if (NT * MINE > 2 || (j & 1)) __builtin_amdgcn_sched_barrier(0);
+            }
+            // four entries of a column t, s = 4 g4 + (0..3), into images of K terms
+            auto put = [&](v4f x, __bf16* to, auto terms) __attribute__((always_inline)) {
+                constexpr int K = decltype(terms)::value;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int ago = 16 * (tb - sb) + c16 - 4 * g4 - i;
-                    const float wgt = MOMENT ? po[ago] * (float)ago : po[ago];
-                    p[i] = ago < 0 ? 0.f : p[i] * wgt;          // not 0 * p: rows after t may hold anything
-                }
-#pragma unroll
-                for (int k = 0; k < TP; ++k) {
-                    const v4bf term = __builtin_convertvector(p, v4bf);
-                    *reinterpret_cast<v4bf*>(pi + (k * C + 16 * tb + c16) * LP + 16 * sb + 4 * g4) = term;
-                    if (k + 1 < TP) {
+                for (int k = 0; k < K; ++k) {
+                    const v4bf term = __builtin_convertvector(x, v4bf);
+                    *reinterpret_cast<v4bf*>(to + k * C * LP) = term;
+                    if (k + 1 < K) {
                         const uint2 u = __builtin_bit_cast(uint2, term);
-                        p -= v4f{bf16_lo(u.x), bf16_hi(u.x), bf16_lo(u.y), bf16_hi(u.y)};
+                        x -= v4f{bf16_lo(u.x), bf16_hi(u.x), bf16_lo(u.y), bf16_hi(u.y)};
                     }
                 }
             };
-#pragma unroll 1
-            for (int n = wave; n < NC * (NC + 1) / 2; n += NW) {
-                const int tb = n < 1 ? 0 : n < 3 ? 1 : n < 6 ? 2 : 3;
-                tile(n - tb * (tb + 1) / 2, tb);
+            const int diagonal = c16 - 4 * g4;
+#pragma unroll
+            for (int y = 0; y < MINE; ++y) {
+                const int to = (16 * tb[y] + c16) * LP + 16 * sb[y] + 4 * g4, ago = 16 * (tb[y] - sb[y]) + diagonal;
+                v4f x = {po[ago], po[ago - 1], po[ago - 2], po[ago - 3]};
+                asm volatile("" : "+v"(x));                 // or a branch goes round each of them
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x[i] = ago - i < 0 ? 0.f : p[y][i] * x[i];      // not 0 * p: rows after t may hold anything
+                put(x, pi + to, Terms<TP>());
+                if constexpr (MOMENT) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) x[i] *= (float)(ago - i);
+                    put(x, mi + to, Terms<3>());
+                }
             }
             from_state();
             __syncthreads();
-        }
 
-        // V's rows 32 kk + 8 g4 + (0..7) of this wave's columns
-        auto column = [&](int kk, v8bf (&v)[NT]) __attribute__((always_inline)) {
+            // tiles 2 t2 and 2 t2 + 1 of the columns of P's images, against 32 kk rows of V
+            auto read_p = [&](const __bf16* img, int kk, int t2, auto& p) __attribute__((always_inline)) {
+                constexpr int K = sizeof(p[0]) / sizeof(v8bf);
 #pragma unroll
-            for (int k = 0; k < NT; ++k)
-                v[k] = lds_turned<W>(vi + (k * C + 32 * kk) * W, v_at);
-        };
-        if constexpr (OUT) {
+                for (int y = 0; y < 2; ++y)
+#pragma unroll
+                    for (int k = 0; k < K; ++k) p[y][k] = lds8(img + (k * C + 32 * t2 + 16 * y + c16) * LP + 32 * kk + 8 * g4);
+            };
+            auto add = [&](const auto& v, const auto& p, auto& to, int t2) __attribute__((always_inline)) {
+                v4f o[NB][2];
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) o[nb][0] = to[nb][2 * t2], o[nb][1] = to[nb][2 * t2 + 1];
+                products(v, p, o);
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) to[nb][2 * t2] = o[nb][0], to[nb][2 * t2 + 1] = o[nb][1];
+            };
 #pragma unroll
             for (int kk = 0; kk < NK; ++kk) {
-                v8bf v[NT];
-                column(kk, v);
-                // rows 32 kk of V meet the tiles of P from 2 kk on
-                v8bf p[2][TP];
+                v8bf v[NB][NT];
+                read_v(kk, v);
 #pragma unroll
                 for (int t2 = kk; t2 < NK; ++t2) {
-#pragma unroll
-                    for (int y = 0; y < 2; ++y)
-#pragma unroll
-                        for (int k = 0; k < TP; ++k) p[y][k] = lds8(pi + (k * C + 32 * t2 + 16 * y + c16) * LP + 32 * kk + 8 * g4);
-                    v4f o[2] = {O[2 * t2], O[2 * t2 + 1]};
-                    products(v, p, o);
-                    O[2 * t2] = o[0], O[2 * t2 + 1] = o[1];
+                    v8bf p[2][TP];
+                    read_p(pi, kk, t2, p);
+                    add(v, p, O, t2);
+                    if constexpr (MOMENT) {
+                        v8bf m[2][TM];
+                        read_p(mi, kk, t2, m);
+                        add(v, m, R, t2);
+                    }
                 }
-                __builtin_amdgcn_sched_barrier(0);
+                if (NT > 1 || MOMENT) __builtin_amdgcn_sched_barrier(0);
             }
             // A row of V that is not finite reaches the rows before it here, as 0 * V.  Then the products are taken again with
             // zeros for such values, and a column that has met one by row t is NaN from there on: the same products count them.
             // The last tile meets all rows of V.
             float probe = 0.f;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) probe = fmaf(O[NC - 1][i], 0.f, probe);
+            for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) probe = fmaf(O[nb][NC - 1][i], 0.f, probe);
             __builtin_amdgcn_sched_barrier(0);
             if (__builtin_expect(__any(probe != 0.f), 0)) {
                 from_state();
+                v4f met[NB][NC];
 #pragma unroll
-                for (int t = 0; t < NC; ++t) {
-                        v4f met = {0.f, 0.f, 0.f, 0.f};
+                for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-                        for (int kk = 0; kk <= t / 2; ++kk) {
-                            v8bf v[NT], p[TP], bad, upto;
-                            column(kk, v);
+                    for (int t = 0; t < NC; ++t) met[nb][t] = v4f{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                            for (int k = 0; k < TP; ++k) p[k] = lds8(pi + (k * C + 16 * t + c16) * LP + 32 * kk + 8 * g4);
+                for (int kk = 0; kk < NK; ++kk) {
+                    v8bf v[NB][NT], bad[NB][1];
+                    read_v(kk, v);
 #pragma unroll
-                            for (int e = 0; e < 8; ++e) {
-                                bool fine = true;
+                    for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-                                for (int k = 0; k < NT; ++k) {
-                                    const bool f = finite32((float)v[k][e]);
-                                    fine = fine && f;
-                                    if (!f) v[k][e] = (__bf16)0.f;
-                                }
-                                bad[e] = fine ? (__bf16)0.f : (__bf16)1.f;
-                                upto[e] = 32 * kk + 8 * g4 + e <= 16 * t + c16 ? (__bf16)1.f : (__bf16)0.f;
+                        for (int e = 0; e < 8; ++e) {
+                            bool fine = true;
+#pragma unroll
+                            for (int k = 0; k < NT; ++k) {
+                                const bool f = finite32((float)v[nb][k][e]);
+                                fine = fine && f;
+                                if (!f) v[nb][k][e] = (__bf16)0.f;
                             }
-                            O[t] = product<NT, TP>(v, p, O[t]);
-                            met = mfma(bad, upto, met);
-                            __builtin_amdgcn_sched_barrier(0);
+                            bad[nb][0][e] = fine ? (__bf16)0.f : (__bf16)1.f;
                         }
 #pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            if (met[i] != 0.f) O[t][i] = __builtin_nanf("");
+                    for (int t2 = kk; t2 < NK; ++t2) {
+                        v8bf p[2][TP], upto[2][1];
+                        read_p(pi, kk, t2, p);
+                        add(v, p, O, t2);
+                        if constexpr (MOMENT) {
+                            v8bf m[2][TM];
+                            read_p(mi, kk, t2, m);
+                            add(v, m, R, t2);
+                        }
+#pragma unroll
+                        for (int y = 0; y < 2; ++y)
+#pragma unroll
+                            for (int e = 0; e < 8; ++e)
+                                upto[y][0][e] = 32 * kk + 8 * g4 + e <= 32 * t2 + 16 * y + c16 ? (__bf16)1.f : (__bf16)0.f;
+                        add(bad, upto, met, t2);
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
                 }
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                    for (int t = 0; t < NC; ++t)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            if (met[nb][t][i] != 0.f) {
+                                O[nb][t][i] = __builtin_nanf("");
+                                if constexpr (MOMENT) R[nb][t][i] = __builtin_nanf("");
+                            }
             }
             float zc = 0.f;
             const char* const outp = outr.at(done);
+            const char* const gradp = gradr.at(done);
 #pragma unroll
-            for (int t = 0; t < NC; ++t) {
-                const int i = 16 * t + c16;
-                const uint32_t at = outr.off(i) + (mycol + 4 * g4) * (BF16 && !(MODE == kOut && w.o_float) ? 2 : 4);
-                if (i < cnt) {
-                    const v4f x = O[t];
-                    if constexpr (MODE == kMoment) {
-                        v4f d;
-                        if constexpr (BF16) {
-                            const uint2 u = *reinterpret_cast<const uint2*>(outp + at);
-                            d = v4f{bf16_lo(u.x), bf16_hi(u.x), bf16_lo(u.y), bf16_hi(u.y)};
-                        } else {
-                            d = *reinterpret_cast<const v4f*>(outp + at);
+            for (int t = 0; t < NC; ++t)
+                if (16 * t + c16 < cnt) {
+                    const bool o_float = !BF16 || w.o_float;
+                    const uint32_t at = outr.off(16 * t + c16) + (mycol + 4 * g4) * (o_float ? 4 : 2);
+#pragma unroll
+                    for (int nb = 0; nb < NB; ++nb) {
+                        char* p = const_cast<char*>(outp + at) + nb * (o_float ? 64 : 32);
+                        if (o_float) *reinterpret_cast<v4f*>(p) = O[nb][t];
+                        else *reinterpret_cast<v4bf*>(p) = __builtin_convertvector(O[nb][t], v4bf);
+                        if constexpr (MODE == kMoment) {
+                            const char* q = gradp + (gradr.off(16 * t + c16) + (mycol + 16 * nb + 4 * g4) * ES);
+                            v4f d;
+                            if constexpr (BF16) {
+                                const uint2 u = *reinterpret_cast<const uint2*>(q);
+                                d = v4f{bf16_lo(u.x), bf16_hi(u.x), bf16_lo(u.y), bf16_hi(u.y)};
+                            } else {
+                                d = *reinterpret_cast<const v4f*>(q);
+                            }
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) zc = fmaf(R[nb][t][e], d[e], zc);
                         }
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) zc = fmaf(x[e], d[e], zc);
-                    } else {
-                        char* p = const_cast<char*>(outp + at);
-                        if (BF16 && !w.o_float) *reinterpret_cast<v4bf*>(p) = __builtin_convertvector(x, v4bf);
-                        else *reinterpret_cast<v4f*>(p) = x;
                     }
                 }
-            }
             if constexpr (MODE == kMoment) z += zc;
         }
 
@@ -491,51 +588,59 @@ decay_chunk_kernel(Walk w) {
         // S <- g^cnt S + K^T diag(g^(cnt-pre-j)) V, and T <- g^cnt (T + cnt S) + ... with the weights' derivative
         const float gc = cnt == C ? gfull : expm1f(lg * (float)cnt);
 #pragma unroll
-            for (int j = 0; j < NJ; ++j)
+        for (int j = 0; j < NJ; ++j)
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
                 for (int a = 0; a < 2; ++a)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         if constexpr (MOMENT) {
-                            const float x = fmaf((float)cnt, S[j][a][i], T[j][a][i]);
-                            T[j][a][i] = fmaf(x, gc, x);
+                            const float x = fmaf((float)cnt, S[j][nb][a][i], T[j][nb][a][i]);
+                            T[j][nb][a][i] = fmaf(x, gc, x);
                         }
-                        S[j][a][i] = fmaf(S[j][a][i], gc, S[j][a][i]);
+                        S[j][nb][a][i] = fmaf(S[j][nb][a][i], gc, S[j][nb][a][i]);
                     }
 #pragma unroll
         for (int kk = 0; kk < NK; ++kk) {
-            v8bf v[3], m[3];
-                v8bf raw[NT];
-                column(kk, raw);
-                v8f x = widen(raw[NT - 1]), y;
-#pragma unroll
-                for (int k = NT - 2; k >= 0; --k) x += widen(raw[k]);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const int left = cnt - pre - (32 * kk + 8 * g4 + e);
-                    x[e] *= pk[left];
-                    if constexpr (MOMENT) y[e] = x[e] * (float)left;
-                }
-                split<3>(x, v);
-                if constexpr (MOMENT) split<3>(y, m);
-#pragma unroll
-            for (int j = 0; j < NJ; ++j) {
-                v8bf kt[2][NT];
+            v8bf kt[2][2][NT];
+            auto read_k = [&](int j) __attribute__((always_inline)) {
 #pragma unroll
                 for (int a = 0; a < 2; ++a)
 #pragma unroll
                     for (int k = 0; k < NT; ++k)
-                        kt[a][k] = lds_turned<D>(ki + (k * C + 32 * kk) * D + 4 * a, kt_at ^ j << 5);
-                products(kt, v, S[j]);
-                if constexpr (MOMENT) products(kt, m, T[j]);
-                if (j & 1) __builtin_amdgcn_sched_barrier(0);
+                        kt[j & 1][a][k] = lds_turned<D>(ki + (k * C + 32 * kk) * D + 4 * a, kt_at ^ (j << 5));
+            };
+            v8bf v[NB][3], m[MB][3], raw[NB][NT];
+            read_v(kk, raw);
+            read_k(0);
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) {
+                v8f x = widen(raw[nb][NT - 1]);
+#pragma unroll
+                for (int k = NT - 2; k >= 0; --k) x += widen(raw[nb][k]);
+                const int left = cnt - pre - (32 * kk + 8 * g4);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[e] *= pk[left - e];
+                split<3>(x, v[nb]);
+                if constexpr (MOMENT) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) x[e] *= (float)(left - e);
+                    split<3>(x, m[nb]);
+                }
             }
-            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) {
+                if (j + 1 < NJ) read_k(j + 1);
+                update(kt[j & 1], v, S[j]);
+                if constexpr (MOMENT) update(kt[j & 1], m, T[j]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
         }
         __syncthreads();        // everybody is done with the images
     }
 
-    if constexpr (MODE == kOut) {
+    if constexpr (OUT) {
         // rows of this part that are not valid
         const int es = BF16 && !w.o_float ? 2 : 4, vecs = W * es / 16;
         for (int i = tid; i < (rows - count) * vecs; i += THREADS) {
@@ -543,28 +648,22 @@ decay_chunk_kernel(Walk w) {
             *reinterpret_cast<v4u*>(p) = v4u{0u, 0u, 0u, 0u};
         }
     }
-    float* to = nullptr;
-    if (STATES) to = w.parts + (((size_t)b * w.H + h) * (w.nparts - 1) + order) * D * D;
-    else if (MODE != kMoment && order == w.nparts - 1 && w.state_out) to = w.state_out + state_at;
-#pragma unroll
-        for (int j = 0; j < NJ; ++j)
-#pragma unroll
-            for (int a = 0; a < 2; ++a)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const size_t at = (size_t)(32 * j + 8 * g4 + 4 * a + i) * D + mycol + c16;
-                    if (to) to[at] = S[j][a][i];
-                    if constexpr (MODE == kMomentState)
-                        w.part_moments[(((size_t)b * w.H + h) * (w.nparts - 1) + order) * D * D + at] = T[j][a][i];
-                    if constexpr (MODE == kMoment)
-                        if (order == w.nparts - 1 && w.grad_state) z += (double)w.grad_state[state_at + at] * T[j][a][i];
-                }
+    float* to = STATES ? w.parts + part_at + (size_t)order * D * D : order == w.nparts - 1 && w.state_out ? w.state_out + state_at : nullptr;
+    if (to) entries([&](uint32_t at, uint32_t, int j, int nb, int a, int i) { to[at] = S[j][nb][a][i]; });
+    if constexpr (MODE == kMomentState)
+        entries([&](uint32_t at, uint32_t, int j, int nb, int a, int i) {
+            w.part_moments[part_at + (size_t)order * D * D + at] = T[j][nb][a][i];
+        });
     if constexpr (MODE == kMoment) {
+        if (order == w.nparts - 1 && w.grad_state)
+            entries([&](uint32_t at, uint32_t across, int j, int nb, int a, int i) {
+                z += (double)w.grad_state[state_at + (w.in_turned ? across : at)] * T[j][nb][a][i];
+            });
 #pragma unroll
         for (int m = 32; m; m >>= 1) z += __shfl_xor(z, m);
         __syncthreads();        // the images are done with, and a part without rows has not come by a barrier
         double* const sum = reinterpret_cast<double*>(lds);
-        if (lane == 0) sum[wave] = z;
+        if ((tid & 63) == 0) sum[wave] = z;
         __syncthreads();
         if (tid == 0) {
             for (int i = 1; i < NW; ++i) z += sum[i];
@@ -628,7 +727,7 @@ hipError_t walk(const Walk& w, hipStream_t stream) {
         e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    if (!w.moment && !w.o.data) return launch<D, BF16, kLast>(w, 1, stream);
+    if (!w.o.data) return launch<D, BF16, kLast>(w, 1, stream);
     return w.moment ? launch<D, BF16, kMoment>(w, w.nparts, stream) : launch<D, BF16, kOut>(w, w.nparts, stream);
 }
 
@@ -643,12 +742,12 @@ hipError_t launch_decay_chunks(const Walk& w, hipStream_t stream) {
     }
 }
 
-int moment_slices(int D) { return D < 128 ? 1 : D / 128; }
+int moment_slices(int D) { return D == 256 ? 4 : 1; }
 
 // Parts that a sequence is cut into.  Two workgroups of the kernel fit a compute unit, so 512 fill the GPU; every part but
 // the last reads K and V once more, so there are no more than that takes, and none below eight chunks of 64 rows.
 DecayParts decay_parts(int B, int N, int H, int D) {
-    const int slices = moment_slices(D);
+    const int slices = D == 256 ? 2 : 1;
     const int64_t have = (int64_t)B * H * slices;
     int64_t n = (512 + have - 1) / have;
     const int64_t most = N / 512;

@@ -40,7 +40,8 @@ struct Walk {
     // [B,H,nparts-1,D,D] work arrays, not used where nparts is 1
     int nparts, part_rows;
     float *parts, *part_moments;
-    // the derivative by log g instead of o: `grad` is the gradient of o, `grad_state` of the last state (or null)
+    // moment: also the derivative of o by log g, summed against `grad`, and that of the last state against `grad_state` (or null;
+    // read transposed with in_turned)
     bool moment;
     Heads grad;
     const float* grad_state;
