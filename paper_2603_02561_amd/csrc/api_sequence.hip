@@ -82,7 +82,7 @@ DecayCarve carve_decay(void* ws, int B, int N, int H, int Hkv, int D, bool backw
         return p;
     };
     if (!backward && N <= kDecayRows) return c;
-    c.cut = decay_parts(B, N, H, D);
+    c.cut = decay_parts(B, N, H, D, backward ? 2 : 1);
     const size_t states = (size_t)B * H * (c.cut.parts - 1) * D * D;
     c.parts = part(states);
     if (backward) {
@@ -201,7 +201,7 @@ solar_status solar_decay_attention(const void* Q, const void* K, const void* V, 
     w.part_rows = c.cut.rows;
     w.parts = c.parts;
     const hipError_t e = N <= kDecayRows ? launch_decay_rows(w, (hipStream_t)stream)
-                                         : launch_decay_chunks(w, (hipStream_t)stream);
+                                         : launch_decay_chunks({{w}, 1}, (hipStream_t)stream);
     return e == hipSuccess ? SOLAR_OK : SOLAR_ERR_HIP;
 }
 
@@ -254,13 +254,13 @@ solar_status solar_decay_attention_backward(const void* Q, const void* K, const 
         a.grad_state = dstate_out;
         a.moments = c.moments;
     }
-    hipError_t e = launch_decay_chunks(a, st);
+    hipError_t e = launch_decay_chunks({{a}, 1}, st);
     if (e != hipSuccess) return SOLAR_ERR_HIP;
     if (dlog_decay) {
         e = launch_moment_sum(c.moments, B, H, c.cut.parts * moment_slices(D), dlog_decay, st);
         if (e != hipSuccess) return SOLAR_ERR_HIP;
     }
-    // dv_t = G_t^T k_t, dk_t = G_t v_t with G_t = scale q_t do_t^T + g G_{t+1}: walks from the last row on
+    // dv_t = G_t^T k_t, dk_t = G_t v_t with G_t = scale q_t do_t^T + g G_{t+1}: walks from the last row on, with one state
     Walk d = w;
     d.reverse = true;
     d.o_scale = 1.f;
@@ -271,13 +271,12 @@ solar_status solar_decay_attention_backward(const void* Q, const void* K, const 
     if (share > 1 && !take(c.dv, nullptr, B, N, H, D, sizeof(float), 1, true, &part)) return SOLAR_ERR_WORKSPACE;
     d.q = k; d.k = q; d.v = g; d.o = share > 1 ? part : dv;
     d.state_out = dstate_in;
-    e = launch_decay_chunks(d, st);
-    if (e != hipSuccess) return SOLAR_ERR_HIP;
+    Walk f = d;
     if (share > 1) part.data = reinterpret_cast<char*>(c.dk);
-    d.q = vv; d.k = g; d.v = q; d.o = share > 1 ? part : dk;
-    d.in_turned = true;
-    d.state_out = nullptr;
-    e = launch_decay_chunks(d, st);
+    f.q = vv; f.k = g; f.v = q; f.o = share > 1 ? part : dk;
+    f.in_turned = f.parts_turned = true;
+    f.state_out = nullptr;
+    e = launch_decay_chunks({{d, f}, 2}, st);
     if (e != hipSuccess) return SOLAR_ERR_HIP;
     if (share > 1) {
         e = launch_share_sum(c.dk, B, N, H, Hkv, D, dk, w.bf16, st);

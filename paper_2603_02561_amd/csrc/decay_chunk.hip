@@ -178,7 +178,7 @@ struct Fetch {
 };
 
 template <int K>
-struct Terms {
+struct Number {
     static constexpr int value = K;
 };
 
@@ -206,11 +206,12 @@ constexpr bool is_out(int mode) { return mode == kOut || mode == kMoment; }
 
 template <int D, bool BF16, int MODE>
 __global__ __launch_bounds__((ChunkCfg<D, BF16, is_moment(MODE)>::kThreads), (ChunkCfg<D, BF16, is_moment(MODE)>::waves(is_out(MODE)))) void
-decay_chunk_kernel(Walk w) {
+decay_chunk_kernel(Walks ws) {
     constexpr bool MOMENT = is_moment(MODE), OUT = is_out(MODE), STATES = MODE == kState || MODE == kMomentState;
     using F = ChunkCfg<D, BF16, MOMENT>;
     constexpr int C = F::C, W = F::W, NB = F::NB, THREADS = F::kThreads, NT = F::NT, TP = F::TP, LP = F::LP;
     constexpr int NW = THREADS / 64, NS = D / W, NJ = D / 32, NC = C / 16, NK = C / 32, ES = BF16 ? 2 : 4;
+    constexpr bool kEarly = OUT && !MOMENT && BF16;
     constexpr int TM = MOMENT ? 3 : 1, MB = MOMENT ? NB : 1, MJ = MOMENT ? NJ : 1;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     __bf16* const ki = reinterpret_cast<__bf16*>(lds);                  // [NT][C][D]
@@ -222,10 +223,11 @@ decay_chunk_kernel(Walk w) {
     float* const pk = pw + C + 1 + C;                                   // kv_scale g^n, n = -C .. C, zero below 0
     float* const po = pk + C + 1 + 16;                                  // o_scale kv_scale g^n, n = -16 .. C, zero below 0
 
-    // Slices of one part and heads that share K and V run on one XCD (workgroups go to the eight in turn), where they
-    // find each other's rows in its L2.
-    const int share = w.k.share, nparts = MODE == kLast ? 1 : STATES ? w.nparts - 1 : w.nparts;
-    const int turn = blockIdx.x >> 3, slice = turn % NS, k0 = turn / NS;
+    // Slices and walks of one part, and heads that share K and V, run on one XCD (workgroups go to the eight in turn), where
+    // they find each other's rows in its L2.
+    const int turn = blockIdx.x >> 3, slice = turn % NS, k0 = turn / NS / ws.count;
+    const Walk& w = ws.walk[turn / NS % ws.count];
+    const int share = ws.walk[0].k.share, nparts = MODE == kLast ? 1 : STATES ? w.nparts - 1 : w.nparts;
     const int64_t unit = (int64_t)(k0 / share * 8 + (blockIdx.x & 7)) * share + k0 % share;
     if (unit >= (int64_t)w.B * w.H * nparts) return;
     const int h = (int)(unit % w.H), b = (int)(unit / w.H / nparts);
@@ -280,7 +282,7 @@ decay_chunk_kernel(Walk w) {
         const bool own = order > 0 && !STATES;          // starts where the part before ends
         const float* start = STATES ? nullptr : own ? w.parts + part_at + (size_t)(order - 1) * D * D
                                                     : w.state_in ? w.state_in + state_at : nullptr;
-        const bool turned = !own && w.in_turned;
+        const bool turned = own ? w.parts_turned : w.in_turned;
         entries([&](uint32_t at, uint32_t across, int j, int nb, int a, int i) {
             S[j][nb][a][i] = start ? start[turned ? across : at] : 0.f;
             if constexpr (MOMENT) T[j][nb][a][i] = own ? w.part_moments[part_at + (size_t)(order - 1) * D * D + at] : 0.f;
@@ -299,12 +301,11 @@ decay_chunk_kernel(Walk w) {
     if constexpr (MODE == kMoment) gradr = Rows<C>::make(row_of(w.grad, b, first, h), step * w.grad.s.row);
     Fetch<C, D, THREADS, BF16> fq, fk;
     Fetch<C, W, THREADS, BF16> fv;
-    auto fetch = [&](int done) __attribute__((always_inline)) {
-        fk.load(kr, done, count);
-        fv.load(vr, done, count);
-        if constexpr (OUT) fq.load(qr, done, count);
-    };
-    if (count) fetch(0);
+    if (count) {
+        fk.load(kr, 0, count);
+        fv.load(vr, 0, count);
+        if constexpr (OUT) fq.load(qr, 0, count);
+    }
 
     // places in the images: chunk g4 of row c16; this lane's four elements of row 8 g4 + c16 / 4 for K^T (columns
     // 8 (c16 % 4) ..) and for V (this wave's columns, 4 (c16 % 4) ..)
@@ -342,8 +343,9 @@ decay_chunk_kernel(Walk w) {
                 for (int k = 0; k < NT; ++k) v[nb][k] = lds_turned<W>(vi + (k * C + 32 * kk) * W, v_at ^ (nb << 4));
         };
         v4f O[NB][NC], R[MB][MOMENT ? NC : 1];
-        // O = Q S times g^(i+pre), R its derivative
-        auto from_state = [&]() __attribute__((always_inline)) {
+        // O = Q S times g^(i+pre), R its derivative; the rows of Q are read a step ahead, or not (for fewer registers)
+        auto from_state = [&](auto ahead) __attribute__((always_inline)) {
+            constexpr int A = decltype(ahead)::value;
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
@@ -351,17 +353,18 @@ decay_chunk_kernel(Walk w) {
                     O[nb][t] = v4f{0.f, 0.f, 0.f, 0.f};
                     if constexpr (MOMENT) R[nb][t] = v4f{0.f, 0.f, 0.f, 0.f};
                 }
-            v8bf q[2][NC][NT];
+            v8bf q[1 + A][NC][NT];
             auto read_q = [&](int j) __attribute__((always_inline)) {
 #pragma unroll
                 for (int t = 0; t < NC; ++t)
 #pragma unroll
-                    for (int k = 0; k < NT; ++k) q[j & 1][t][k] = lds8(qi + (k * C + 16 * t) * D + (row_at ^ (j << 5)));
+                    for (int k = 0; k < NT; ++k) q[j & A][t][k] = lds8(qi + (k * C + 16 * t) * D + (row_at ^ (j << 5)));
             };
-            read_q(0);
+            if (A) read_q(0);
 #pragma unroll
             for (int j = 0; j < NJ; ++j) {
-                if (j + 1 < NJ) read_q(j + 1);
+                if (!A) read_q(j);
+                else if (j + 1 < NJ) read_q(j + 1);
                 v8bf s[NB][TP];
 #pragma unroll
                 for (int nb = 0; nb < NB; ++nb) {
@@ -370,7 +373,7 @@ decay_chunk_kernel(Walk w) {
                     for (int e = 0; e < 8; ++e) x[e] = S[j][nb][e / 4][e % 4];
                     split<TP>(x, s[nb]);
                 }
-                products(s, q[j & 1], O);
+                products(s, q[j & A], O);
                 if constexpr (MOMENT) {
                     v8bf m[NB][3];
 #pragma unroll
@@ -380,7 +383,7 @@ decay_chunk_kernel(Walk w) {
                         for (int e = 0; e < 8; ++e) x[e] = T[j][nb][e / 4][e % 4];
                         split<3>(x, m[nb]);
                     }
-                    products(m, q[j & 1], R);
+                    products(m, q[j & A], R);
                 }
                 // or the operands of all steps are read at once, and registers spilled
                 __builtin_amdgcn_sched_barrier(0);
@@ -446,15 +449,19 @@ decay_chunk_kernel(Walk w) {
                 asm volatile("" : "+v"(x));                 // or a branch goes round each of them
 #pragma unroll
                 for (int i = 0; i < 4; ++i) x[i] = ago - i < 0 ? 0.f : p[y][i] * x[i];      // not 0 * p: rows after t may hold anything
-                put(x, pi + to, Terms<TP>());
+                put(x, pi + to, Number<TP>());
                 if constexpr (MOMENT) {
 #pragma unroll
                     for (int i = 0; i < 4; ++i) x[i] *= (float)(ago - i);
-                    put(x, mi + to, Terms<3>());
+                    put(x, mi + to, Number<3>());
                 }
             }
-            from_state();
+            from_state(Number<1>());
             __syncthreads();
+            if (kEarly) {
+                fk.load(kr, done + C, count);
+                fq.load(qr, done + C, count);
+            }
 
             // tiles 2 t2 and 2 t2 + 1 of the columns of P's images, against 32 kk rows of V
             auto read_p = [&](const __bf16* img, int kk, int t2, auto& p) __attribute__((always_inline)) {
@@ -499,32 +506,29 @@ decay_chunk_kernel(Walk w) {
                 for (int i = 0; i < 4; ++i) probe = fmaf(O[nb][NC - 1][i], 0.f, probe);
             __builtin_amdgcn_sched_barrier(0);
             if (__builtin_expect(__any(probe != 0.f), 0)) {
-                from_state();
-                v4f met[NB][NC];
+                from_state(Number<0>());
 #pragma unroll
-                for (int nb = 0; nb < NB; ++nb)
+                for (int t2 = 0; t2 < NK; ++t2) {
+                    v4f met[NB][2];
 #pragma unroll
-                    for (int t = 0; t < NC; ++t) met[nb][t] = v4f{0.f, 0.f, 0.f, 0.f};
+                    for (int nb = 0; nb < NB; ++nb) met[nb][0] = met[nb][1] = v4f{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int kk = 0; kk < NK; ++kk) {
-                    v8bf v[NB][NT], bad[NB][1];
-                    read_v(kk, v);
+                    for (int kk = 0; kk <= t2; ++kk) {
+                        v8bf v[NB][NT], bad[NB][1], p[2][TP], upto[2][1];
+                        read_v(kk, v);
 #pragma unroll
-                    for (int nb = 0; nb < NB; ++nb)
+                        for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            bool fine = true;
+                            for (int e = 0; e < 8; ++e) {
+                                bool fine = true;
 #pragma unroll
-                            for (int k = 0; k < NT; ++k) {
-                                const bool f = finite32((float)v[nb][k][e]);
-                                fine = fine && f;
-                                if (!f) v[nb][k][e] = (__bf16)0.f;
+                                for (int k = 0; k < NT; ++k) {
+                                    const bool f = finite32((float)v[nb][k][e]);
+                                    fine = fine && f;
+                                    if (!f) v[nb][k][e] = (__bf16)0.f;
+                                }
+                                bad[nb][0][e] = fine ? (__bf16)0.f : (__bf16)1.f;
                             }
-                            bad[nb][0][e] = fine ? (__bf16)0.f : (__bf16)1.f;
-                        }
-#pragma unroll
-                    for (int t2 = kk; t2 < NK; ++t2) {
-                        v8bf p[2][TP], upto[2][1];
                         read_p(pi, kk, t2, p);
                         add(v, p, O, t2);
                         if constexpr (MOMENT) {
@@ -537,20 +541,20 @@ decay_chunk_kernel(Walk w) {
 #pragma unroll
                             for (int e = 0; e < 8; ++e)
                                 upto[y][0][e] = 32 * kk + 8 * g4 + e <= 32 * t2 + 16 * y + c16 ? (__bf16)1.f : (__bf16)0.f;
-                        add(bad, upto, met, t2);
+                        products(bad, upto, met);
                         __builtin_amdgcn_sched_barrier(0);
                     }
+#pragma unroll
+                    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                        for (int y = 0; y < 2; ++y)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i)
+                                if (met[nb][y][i] != 0.f) {
+                                    O[nb][2 * t2 + y][i] = __builtin_nanf("");
+                                    if constexpr (MOMENT) R[nb][2 * t2 + y][i] = __builtin_nanf("");
+                                }
                 }
-#pragma unroll
-                for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-                    for (int t = 0; t < NC; ++t)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            if (met[nb][t][i] != 0.f) {
-                                O[nb][t][i] = __builtin_nanf("");
-                                if constexpr (MOMENT) R[nb][t][i] = __builtin_nanf("");
-                            }
             }
             float zc = 0.f;
             const char* const outp = outr.at(done);
@@ -583,7 +587,11 @@ decay_chunk_kernel(Walk w) {
         }
 
         // the next rows are on their way while S is updated, where registers are free for them
-        fetch(done + C);
+        if (!kEarly) {
+            fk.load(kr, done + C, count);
+            if constexpr (OUT) fq.load(qr, done + C, count);
+        }
+        fv.load(vr, done + C, count);
 
         // S <- g^cnt S + K^T diag(g^(cnt-pre-j)) V, and T <- g^cnt (T + cnt S) + ... with the weights' derivative
         const float gc = cnt == C ? gfull : expm1f(lg * (float)cnt);
@@ -702,24 +710,28 @@ __global__ __launch_bounds__(kJoinThreads) void join_parts_kernel(Walk w) {
 }
 
 template <int D, bool BF16, int MODE>
-hipError_t launch(const Walk& w, int parts, hipStream_t stream) {
+hipError_t launch(const Walks& ws, int parts, hipStream_t stream) {
     using F = ChunkCfg<D, BF16, is_moment(MODE)>;
     auto kern = decay_chunk_kernel<D, BF16, MODE>;
     constexpr size_t bytes = F::lds_bytes(is_out(MODE));
     hipError_t e = allow_dynamic_lds(reinterpret_cast<const void*>(kern), bytes);
     if (e != hipSuccess) return e;
+    const Walk& w = ws.walk[0];
     const int share = w.k.share;
     const int64_t groups = (int64_t)w.B * w.H * parts / share;
-    const int64_t blocks = (groups + 7) / 8 * 8 * share * (D / F::W);
-    hipLaunchKernelGGL(kern, dim3((unsigned)blocks), dim3(F::kThreads), bytes, stream, w);
+    const int64_t blocks = (groups + 7) / 8 * 8 * share * ws.count * (D / F::W);
+    hipLaunchKernelGGL(kern, dim3((unsigned)blocks), dim3(F::kThreads), bytes, stream, ws);
     return hipGetLastError();
 }
 
 template <int D, bool BF16>
-hipError_t walk(const Walk& w, hipStream_t stream) {
+hipError_t run(const Walks& ws, hipStream_t stream) {
+    const Walk& w = ws.walk[0];
     hipError_t e;
     if (w.nparts > 1) {
-        e = w.moment ? launch<D, BF16, kMomentState>(w, w.nparts - 1, stream) : launch<D, BF16, kState>(w, w.nparts - 1, stream);
+        Walks one = ws;
+        one.count = 1;
+        e = w.moment ? launch<D, BF16, kMomentState>(one, w.nparts - 1, stream) : launch<D, BF16, kState>(one, w.nparts - 1, stream);
         if (e != hipSuccess) return e;
         const dim3 grid((unsigned)((size_t)w.B * w.H * D * D / kJoinThreads));
         if (w.moment) hipLaunchKernelGGL(join_parts_kernel<true>, grid, dim3(kJoinThreads), 0, stream, w);
@@ -727,17 +739,18 @@ hipError_t walk(const Walk& w, hipStream_t stream) {
         e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    if (!w.o.data) return launch<D, BF16, kLast>(w, 1, stream);
-    return w.moment ? launch<D, BF16, kMoment>(w, w.nparts, stream) : launch<D, BF16, kOut>(w, w.nparts, stream);
+    if (!w.o.data) return launch<D, BF16, kLast>(ws, 1, stream);
+    return w.moment ? launch<D, BF16, kMoment>(ws, w.nparts, stream) : launch<D, BF16, kOut>(ws, w.nparts, stream);
 }
 
 }  // namespace
 
-hipError_t launch_decay_chunks(const Walk& w, hipStream_t stream) {
+hipError_t launch_decay_chunks(const Walks& ws, hipStream_t stream) {
+    const Walk& w = ws.walk[0];
     switch (w.D) {
-        case 64: return w.bf16 ? walk<64, true>(w, stream) : walk<64, false>(w, stream);
-        case 128: return w.bf16 ? walk<128, true>(w, stream) : walk<128, false>(w, stream);
-        case 256: return w.bf16 ? walk<256, true>(w, stream) : walk<256, false>(w, stream);
+        case 64: return w.bf16 ? run<64, true>(ws, stream) : run<64, false>(ws, stream);
+        case 128: return w.bf16 ? run<128, true>(ws, stream) : run<128, false>(ws, stream);
+        case 256: return w.bf16 ? run<256, true>(ws, stream) : run<256, false>(ws, stream);
         default: return hipErrorInvalidValue;
     }
 }
@@ -745,12 +758,12 @@ hipError_t launch_decay_chunks(const Walk& w, hipStream_t stream) {
 int moment_slices(int D) { return D == 256 ? 4 : 1; }
 
 // Parts that a sequence is cut into.  Two workgroups of the kernel fit a compute unit, so 512 fill the GPU; every part but
-// the last reads K and V once more, so there are no more than that takes, and none below eight chunks of 64 rows.
-DecayParts decay_parts(int B, int N, int H, int D) {
-    const int slices = D == 256 ? 2 : 1;
-    const int64_t have = (int64_t)B * H * slices;
+// the last reads K and V once more, so there are no more than that takes, and none below 128 rows.  `walks` of them run in one
+// launch.
+DecayParts decay_parts(int B, int N, int H, int D, int walks) {
+    const int64_t have = (int64_t)B * H * (D == 256 ? 2 : 1) * walks;
     int64_t n = (512 + have - 1) / have;
-    const int64_t most = N / 512;
+    const int64_t most = N / 128;
     if (n > most) n = most;
     if (n < 1) n = 1;
     const int rows = (int)((((int64_t)N + n - 1) / n + 63) / 64 * 64);

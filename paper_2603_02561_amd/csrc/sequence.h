@@ -40,12 +40,20 @@ struct Walk {
     // [B,H,nparts-1,D,D] work arrays, not used where nparts is 1
     int nparts, part_rows;
     float *parts, *part_moments;
+    bool parts_turned;              // parts hold the states of this walk transposed
     // moment: also the derivative of o by log g, summed against `grad`, and that of the last state against `grad_state` (or null;
     // read transposed with in_turned)
     bool moment;
     Heads grad;
     const float* grad_state;
     double* moments;                // [B][H][nparts][moment_slices(D)] partial sums
+};
+
+// Walks that run side by side: users, rows, heads, types and parts are the same, and the states of the first (in `parts`) are
+// those of all.
+struct Walks {
+    Walk walk[2];
+    int count;
 };
 
 // decay.hip
@@ -62,9 +70,9 @@ hipError_t launch_share_sum(const float* in, int B, int N, int H, int Hkv, int D
 struct DecayParts {
     int parts, rows;
 };
-DecayParts decay_parts(int B, int N, int H, int D);
+DecayParts decay_parts(int B, int N, int H, int D, int walks);
 int moment_slices(int D);
-hipError_t launch_decay_chunks(const Walk& w, hipStream_t stream);
+hipError_t launch_decay_chunks(const Walks& ws, hipStream_t stream);
 
 // rotary.hip
 struct Rotary {
