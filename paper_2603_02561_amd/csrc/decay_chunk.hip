@@ -41,6 +41,15 @@ struct ChunkCfg {
 };
 
 typedef float v8f __attribute__((ext_vector_type(8)));
+typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
+
+// x minus one of a pair of bf16: in one instruction, and exact where that is x rounded.  The pair (-1, 0) comes from a register:
+// as an inline constant the instruction reads -1.0 as (0, -1).
+__device__ __forceinline__ float minus(float x, v2bf pair, int which) {
+    uint32_t one = which ? 0xbf800000u : 0x0000bf80u;
+    asm("" : "+s"(one));
+    return __builtin_amdgcn_fdot2_f32_bf16(pair, __builtin_bit_cast(v2bf, one), x, false);
+}
 
 // The float that a bf16 stands for, from pairs in a register: converted one by one the compiler takes every conversion twice.
 __device__ __forceinline__ v8f widen(v8bf x) {
@@ -54,13 +63,24 @@ __device__ __forceinline__ v8f widen(v8bf x) {
     return f;
 }
 
-// x = the sum of its terms, to 8 bits each
+// x = the sum of its terms, to 8 bits each.  A neighbour that is not finite makes both of a pair NaN.
 template <int T>
 __device__ __forceinline__ void split(v8f x, v8bf (&s)[T]) {
 #pragma unroll
     for (int k = 0; k < T; ++k) {
         s[k] = __builtin_convertvector(x, v8bf);
-        if (k + 1 < T) x -= widen(s[k]);
+        if (k + 1 < T)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = minus(x[e], v2bf{s[k][e & ~1], s[k][e | 1]}, e & 1);
+    }
+}
+
+// The same where neighbours must not meet: they are columns of an input.
+__device__ __forceinline__ void split_apart(v8f x, v8bf (&s)[3]) {
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+        s[k] = __builtin_convertvector(x, v8bf);
+        if (k < 2) x -= widen(s[k]);
     }
 }
 
@@ -160,7 +180,7 @@ struct Fetch {
                 v8bf s[3];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) f[e] = __uint_as_float(x[u][e / 4][e % 4]);
-                split<3>(f, s);
+                split_apart(f, s);
 #pragma unroll
                 for (int k = 0; k < 3; ++k) *reinterpret_cast<v8bf*>(to + k * C * COLS) = s[k];
             }
@@ -435,10 +455,9 @@ decay_chunk_kernel(Walks ws) {
                 for (int k = 0; k < K; ++k) {
                     const v4bf term = __builtin_convertvector(x, v4bf);
                     *reinterpret_cast<v4bf*>(to + k * C * LP) = term;
-                    if (k + 1 < K) {
-                        const uint2 u = __builtin_bit_cast(uint2, term);
-                        x -= v4f{bf16_lo(u.x), bf16_hi(u.x), bf16_lo(u.y), bf16_hi(u.y)};
-                    }
+                    if (k + 1 < K)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) x[i] = minus(x[i], v2bf{term[i & ~1], term[i | 1]}, i & 1);
                 }
             };
             const int diagonal = c16 - 4 * g4;
