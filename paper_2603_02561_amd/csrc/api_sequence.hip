@@ -289,7 +289,7 @@ solar_status solar_decay_attention_backward(const void* Q, const void* K, const 
 
 static solar_status check_norm(int rows, int groups, int d) {
     if (rows <= 0 || groups <= 0 || d <= 0) return SOLAR_ERR_INVALID_ARG;
-    if (d > kNormMaxD || (int64_t)groups * d > (1 << 28) || (int64_t)rows * groups > INT_MAX) return SOLAR_ERR_UNSUPPORTED;
+    if (d > kNormMaxD || groups > 1 << 20 || (int64_t)groups * d > (1 << 28) || (int64_t)rows * groups > INT_MAX) return SOLAR_ERR_UNSUPPORTED;
     return SOLAR_OK;
 }
 

@@ -4,16 +4,17 @@
 //
 // Bound by memory: x is read once and y written once; the gradient reads x and dy once and writes dx once.  A row stays
 // in registers, so mean and variance are taken one after the other from the same values (no difference of two large
-// sums).  Between 8 and 256 threads share a row, by its width; each such team walks over rows a whole number of groups
-// apart, so that its weights, and its sums for dw and db, stay in registers.  The teams' sums go to the workspace and are
-// added by a second kernel in a fixed order.
+// sums).  Between 8 and 1024 threads share a row, by its width; each such team walks over rows of one group, the next of them
+// on its way, so that its weights, and its sums for dw and db, stay in registers.  The sums of a workgroup go to the workspace
+// and are added by a second kernel in a fixed order.
 #include "sequence.h"
 
 namespace solar {
 
 namespace {
 
-constexpr int kThreads = 256;
+// Threads of a workgroup whose rows take T threads each.
+constexpr int block_for(int T) { return T < 256 ? 256 : T; }
 
 template <bool BF16>
 struct Elem {
@@ -31,43 +32,45 @@ __device__ __forceinline__ int column(int t, int v, int e) {
     return VEC ? (v * T + t) * 8 + e : (v * 8 + e) * T + t;
 }
 
-// A team's part of one row; what lies past d is zero.
+// A team's part of one row as it comes from memory; what lies past d is zero.
 template <int T, int NV, bool VEC, bool BF16>
-__device__ __forceinline__ void load_row(const void* base, size_t at, int d, int t, float (&x)[NV][8]) {
-    using E = typename Elem<BF16>::type;
-    const E* p = reinterpret_cast<const E*>(base) + at;
+struct Row {
+    static constexpr int VS = BF16 ? 1 : 2;     // 16-byte loads of eight elements
+    v4u raw[VEC ? NV : 1][VS];
+    float one[VEC ? 1 : NV][8];
+
+    __device__ __forceinline__ void load(const void* base, size_t at, int d, int t) {
+        using E = typename Elem<BF16>::type;
+        const E* p = reinterpret_cast<const E*>(base) + at;
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
-        if constexpr (VEC) {
-            const int c = column<T, VEC>(t, v, 0);
+        for (int v = 0; v < NV; ++v) {
+            if constexpr (VEC) {
+                const int c = column<T, VEC>(t, v, 0);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[v][e] = 0.f;
-            if (c < d) {
-                if constexpr (BF16) {
-                    const v4u u = *reinterpret_cast<const v4u*>(p + c);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        x[v][2 * e] = bf16_lo(u[e]);
-                        x[v][2 * e + 1] = bf16_hi(u[e]);
-                    }
-                } else {
-#pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-                        const v4f u = reinterpret_cast<const v4f*>(p + c)[j];
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) x[v][4 * j + e] = u[e];
-                    }
+                for (int j = 0; j < VS; ++j) {
+                    raw[v][j] = v4u{0u, 0u, 0u, 0u};
+                    if (c < d) raw[v][j] = reinterpret_cast<const v4u*>(p + c)[j];
                 }
-            }
-        } else {
+            } else {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int c = column<T, VEC>(t, v, e);
-                x[v][e] = c < d ? (float)p[c] : 0.f;
+                for (int e = 0; e < 8; ++e) {
+                    const int c = column<T, VEC>(t, v, e);
+                    one[v][e] = c < d ? (float)p[c] : 0.f;
+                }
             }
         }
     }
-}
+    __device__ __forceinline__ void get(float (&x)[NV][8]) const {
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                if constexpr (!VEC) x[v][e] = one[v][e];
+                else if constexpr (BF16) x[v][e] = e & 1 ? bf16_hi(raw[v][0][e / 2]) : bf16_lo(raw[v][0][e / 2]);
+                else x[v][e] = __uint_as_float(raw[v][e / 4][e % 4]);
+            }
+    }
+};
 
 template <int T, int NV, bool VEC, bool BF16>
 __device__ __forceinline__ void store_row(void* base, size_t at, int d, int t, const float (&x)[NV][8]) {
@@ -104,7 +107,7 @@ __device__ __forceinline__ void store_row(void* base, size_t at, int d, int t, c
 // Sums of K values over a team, in every thread of it.  `turn` alternates between the two halves of `part`, so that one
 // barrier a call is enough.
 template <int T, int K>
-__device__ __forceinline__ void team_sum(float (&s)[K], float (*part)[4][K], int& turn) {
+__device__ __forceinline__ void team_sum(float (&s)[K], float (*part)[16][K], int& turn) {
 #pragma unroll
     for (int m = 1; m < (T < 64 ? T : 64); m <<= 1)
 #pragma unroll
@@ -116,20 +119,24 @@ __device__ __forceinline__ void team_sum(float (&s)[K], float (*part)[4][K], int
             for (int k = 0; k < K; ++k) part[turn][wave][k] = s[k];
         __syncthreads();
 #pragma unroll
-        for (int k = 0; k < K; ++k) s[k] = part[turn][0][k] + part[turn][1][k] + part[turn][2][k] + part[turn][3][k];
+        for (int k = 0; k < K; ++k) {
+            s[k] = part[turn][0][k];
+#pragma unroll
+            for (int y = 1; y < T / 64; ++y) s[k] += part[turn][y][k];
+        }
         turn ^= 1;
     }
 }
 
 // `teams` teams, a multiple of `groups`, walk over `rows` rows of d elements (groups counted as rows).
 template <int T, int NV, bool VEC, bool IN_BF16, bool OUT_BF16>
-__global__ __launch_bounds__(kThreads) void layer_norm_kernel(const void* in, const float* __restrict__ weight,
+__global__ __launch_bounds__(block_for(T)) void layer_norm_kernel(const void* in, const float* __restrict__ weight,
                                                               const float* __restrict__ bias, size_t rows, int groups,
                                                               int teams, int d, float eps, void* out, float* mean,
                                                               float* rstd) {
-    __shared__ float part[2][4][1];
+    __shared__ float part[2][16][1];
     int turn = 0;
-    const int t = threadIdx.x % T, team = blockIdx.x * (kThreads / T) + threadIdx.x / T;
+    const int t = threadIdx.x % T, team = blockIdx.x * (block_for(T) / T) + threadIdx.x / T;
     if (team >= teams) return;      // whole workgroups where a team is one
     const int group = team % groups;
     float w[NV][8], b[NV][8];
@@ -142,9 +149,12 @@ __global__ __launch_bounds__(kThreads) void layer_norm_kernel(const void* in, co
             b[v][e] = bias && c < d ? bias[(size_t)group * d + c] : 0.f;
         }
     const float inv = 1.f / (float)d;
+    Row<T, NV, VEC, IN_BF16> next;
+    next.load(in, (size_t)team * d, d, t);
     for (size_t row = team; row < rows; row += teams) {
         float x[NV][8];
-        load_row<T, NV, VEC, IN_BF16>(in, row * d, d, t, x);
+        next.get(x);
+        if (row + teams < rows) next.load(in, (row + teams) * d, d, t);
         float s[1] = {0.f};
 #pragma unroll
         for (int v = 0; v < NV; ++v)
@@ -174,16 +184,18 @@ __global__ __launch_bounds__(kThreads) void layer_norm_kernel(const void* in, co
     }
 }
 
-// partials [2][teams][d]: sums of dy xh and of dy of each team; null where neither is wanted
+// A workgroup takes rows of one group, blockIdx.x % groups, its teams one each at a time.  partials [2][blocks / groups][groups]
+// [d]: its sums of dy xh and of dy; null where neither is wanted.
 template <int T, int NV, bool VEC, bool IN_BF16, bool DOUT_BF16>
-__global__ __launch_bounds__(kThreads) void layer_norm_backward_kernel(
+__global__ __launch_bounds__(block_for(T)) void layer_norm_backward_kernel(
     const void* in, const float* __restrict__ weight, const float* __restrict__ mean, const float* __restrict__ rstd,
-    const void* dout, size_t rows, int groups, int teams, int d, void* din, float* partials) {
-    __shared__ float part[2][4][2];
+    const void* dout, size_t rows, int groups, int d, void* din, float* partials) {
+    constexpr int TEAMS = block_for(T) / T;
+    __shared__ float part[2][16][2];
+    __shared__ float sums[TEAMS > 1 ? TEAMS : 1][TEAMS > 1 ? T * NV * 8 : 1];
     int turn = 0;
-    const int t = threadIdx.x % T, team = blockIdx.x * (kThreads / T) + threadIdx.x / T;
-    if (team >= teams) return;
-    const int group = team % groups;
+    const int t = threadIdx.x % T, team = threadIdx.x / T;
+    const int group = blockIdx.x % groups, block = blockIdx.x / groups, blocks = gridDim.x / groups;
     float w[NV][8], dw[NV][8], db[NV][8];
 #pragma unroll
     for (int v = 0; v < NV; ++v)
@@ -194,11 +206,25 @@ __global__ __launch_bounds__(kThreads) void layer_norm_backward_kernel(
             dw[v][e] = db[v][e] = 0.f;
         }
     const float inv = 1.f / (float)d;
-    for (size_t row = team; row < rows; row += teams) {
+    const size_t step = (size_t)blocks * TEAMS;
+    size_t i = (size_t)block * TEAMS + team;
+    Row<T, NV, VEC, IN_BF16> nx;
+    Row<T, NV, VEC, DOUT_BF16> ny;
+    float mu_next = 0.f, rs_next = 0.f;
+    auto fetch = [&](size_t r) __attribute__((always_inline)) {
+        const size_t row = r * groups + group;
+        nx.load(in, row * d, d, t);
+        ny.load(dout, row * d, d, t);
+        mu_next = mean[row];
+        rs_next = rstd[row];
+    };
+    if (i < rows) fetch(i);
+    for (; i < rows; i += step) {
         float x[NV][8], dy[NV][8];
-        load_row<T, NV, VEC, IN_BF16>(in, row * d, d, t, x);
-        load_row<T, NV, VEC, DOUT_BF16>(dout, row * d, d, t, dy);
-        const float mu = mean[row], rs = rstd[row];
+        nx.get(x);
+        ny.get(dy);
+        const float mu = mu_next, rs = rs_next;
+        if (i + step < rows) fetch(i + step);
         float s[2] = {0.f, 0.f};
 #pragma unroll
         for (int v = 0; v < NV; ++v)
@@ -218,31 +244,48 @@ __global__ __launch_bounds__(kThreads) void layer_norm_backward_kernel(
         for (int v = 0; v < NV; ++v)
 #pragma unroll
             for (int e = 0; e < 8; ++e) x[v][e] = rs * (fmaf(dy[v][e], w[v][e], -m0) - x[v][e] * m1);
-        store_row<T, NV, VEC, IN_BF16>(din, row * d, d, t, x);
+        store_row<T, NV, VEC, IN_BF16>(din, (i * groups + group) * d, d, t, x);
     }
-    if (partials) {
-        store_row<T, NV, VEC, false>(partials, (size_t)team * d, d, t, dw);
-        store_row<T, NV, VEC, false>(partials, ((size_t)teams + team) * d, d, t, db);
+    if (!partials) return;
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+        float* out = partials + (((size_t)which * blocks + block) * groups + group) * d;
+        const float(&mine)[NV][8] = which ? db : dw;
+        if constexpr (TEAMS == 1) {
+            store_row<T, NV, VEC, false>(out, 0, d, t, mine);
+        } else {
+            __syncthreads();
+#pragma unroll
+            for (int v = 0; v < NV; ++v)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sums[team][column<T, VEC>(t, v, e)] = mine[v][e];
+            __syncthreads();
+            for (int c = threadIdx.x; c < d; c += block_for(T)) {
+                float s = 0.f;
+                for (int y = 0; y < TEAMS; ++y) s += sums[y][c];
+                out[c] = s;
+            }
+        }
     }
 }
 
-// dweight and dbias [width] from [2][n][width]: 64 columns a workgroup, 16 of its threads down each
+// dweight and dbias [width] from [2][n][width]: 32 columns a workgroup, 32 of its threads down each
 __global__ __launch_bounds__(1024) void norm_sum_kernel(const float* __restrict__ partials, int n, int width, float* dweight,
                                                         float* dbias) {
-    __shared__ float sum[16][64];
-    const int x = threadIdx.x & 63, y = threadIdx.x >> 6, c = blockIdx.x * 64 + x;
+    __shared__ float sum[32][33];
+    const int x = threadIdx.x & 31, y = threadIdx.x >> 5, c = blockIdx.x * 32 + x;
     float* out = blockIdx.y ? dbias : dweight;
     if (!out) return;
     const float* p = partials + (size_t)blockIdx.y * n * width;
     float s = 0.f;
     if (c < width)
-        for (int i = y; i < n; i += 16) s += p[(size_t)i * width + c];
+        for (int i = y; i < n; i += 32) s += p[(size_t)i * width + c];
     sum[y][x] = s;
     __syncthreads();
-    if (y == 0 && c < width) {
-        for (int i = 1; i < 16; ++i) s += sum[i][x];
-        out[c] = s;
-    }
+    s = sum[x][y];              // column y of the workgroup, row x of the sums
+#pragma unroll
+    for (int m = 16; m; m >>= 1) s += __shfl_xor(s, m);
+    if (x == 0 && blockIdx.x * 32 + y < width) out[blockIdx.x * 32 + y] = s;
 }
 
 // Threads a row, and vectors a thread: a row of up to 512 elements stays in a wave at one vector a thread.
@@ -258,21 +301,29 @@ Team team_for(int d) {
     if (d <= 1024) return {64, 2};
     if (d <= 2048) return {256, 1};
     if (d <= 4096) return {256, 2};
-    if (d <= 8192) return {256, 4};
-    return {256, 8};
+    if (d <= 8192) return {512, 2};
+    return {1024, 2};
 }
 
-// Teams: four workgroups for each compute unit, whole groups, no team without a row.
+// Teams of the forward pass: four workgroups for each compute unit, whole groups, no team without a row.
 int teams_for(int rows, int groups, int d) {
-    const int per_block = kThreads / team_for(d).threads;
+    const int per_block = block_for(team_for(d).threads) / team_for(d).threads;
     const size_t all = (size_t)rows * groups, want = (size_t)1024 * per_block;
     const size_t teams = (want + groups - 1) / groups * groups;
     return (int)(teams < all ? teams : all);
 }
 
+// Workgroups of the gradient for each group: their sums for dw and db are written once each, so there are no more than keep
+// the GPU busy (1024 together), and none whose teams would have less than four rows.
+int blocks_for(int rows, int groups, int d) {
+    const int per_block = block_for(team_for(d).threads) / team_for(d).threads;
+    const int want = ceil_div(1024, groups), most = ceil_div(rows, 4 * per_block);
+    return want < most ? want : most;
+}
+
 }  // namespace
 
-size_t norm_partial_floats(int rows, int groups, int d) { return (size_t)2 * teams_for(rows, groups, d) * d; }
+size_t norm_partial_floats(int rows, int groups, int d) { return (size_t)2 * blocks_for(rows, groups, d) * groups * d; }
 
 #define SOLAR_NORM_SHAPES(CALL)                                  \
     switch (tm.threads * 16 + tm.vectors) {                      \
@@ -283,8 +334,8 @@ size_t norm_partial_floats(int rows, int groups, int d) { return (size_t)2 * tea
         case 64 * 16 + 2: CALL(64, 2); break;                    \
         case 256 * 16 + 1: CALL(256, 1); break;                  \
         case 256 * 16 + 2: CALL(256, 2); break;                  \
-        case 256 * 16 + 4: CALL(256, 4); break;                  \
-        case 256 * 16 + 8: CALL(256, 8); break;                  \
+        case 512 * 16 + 2: CALL(512, 2); break;                  \
+        case 1024 * 16 + 2: CALL(1024, 2); break;                \
         default: return hipErrorInvalidValue;                    \
     }
 
@@ -295,7 +346,8 @@ hipError_t forward(const void* in, const float* weight, const float* bias, int r
                    void* out, float* mean, float* rstd, hipStream_t stream) {
     const Team tm = team_for(d);
     const int teams = teams_for(rows, groups, d);
-    const dim3 grid(ceil_div(teams, kThreads / tm.threads)), block(kThreads);
+    const int threads = block_for(tm.threads);
+    const dim3 grid(ceil_div(teams, threads / tm.threads)), block(threads);
 #define SOLAR_CALL(T, NV)                                                                                        \
     hipLaunchKernelGGL((layer_norm_kernel<T, NV, VEC, A, B>), grid, block, 0, stream, in, weight, bias,          \
                        (size_t)rows * groups, groups, teams, d, eps, out, mean, rstd)
@@ -308,11 +360,10 @@ template <bool VEC, bool A, bool B>
 hipError_t backward(const void* in, const float* weight, const float* mean, const float* rstd, const void* dout, int rows,
                     int groups, int d, void* din, float* partials, hipStream_t stream) {
     const Team tm = team_for(d);
-    const int teams = teams_for(rows, groups, d);
-    const dim3 grid(ceil_div(teams, kThreads / tm.threads)), block(kThreads);
-#define SOLAR_CALL(T, NV)                                                                                          \
+    const dim3 grid((unsigned)blocks_for(rows, groups, d) * groups), block(block_for(tm.threads));
+#define SOLAR_CALL(T, NV)                                                                                              \
     hipLaunchKernelGGL((layer_norm_backward_kernel<T, NV, VEC, A, B>), grid, block, 0, stream, in, weight, mean, rstd, \
-                       dout, (size_t)rows * groups, groups, teams, d, din, partials)
+                       dout, (size_t)rows, groups, d, din, partials)
     SOLAR_NORM_SHAPES(SOLAR_CALL)
 #undef SOLAR_CALL
     return hipGetLastError();
@@ -346,8 +397,8 @@ hipError_t launch_layer_norm_backward(const void* in, const float* weight, const
 #undef SOLAR_NORM
     if (e != hipSuccess || !part) return e;
     const int width = groups * d;
-    hipLaunchKernelGGL(norm_sum_kernel, dim3(ceil_div(width, 64), 2), dim3(1024), 0, stream, partials,
-                       teams_for(rows, groups, d) / groups, width, dweight, dbias);
+    hipLaunchKernelGGL(norm_sum_kernel, dim3(ceil_div(width, 32), 2), dim3(1024), 0, stream, partials,
+                       blocks_for(rows, groups, d), width, dweight, dbias);
     return hipGetLastError();
 }
 
