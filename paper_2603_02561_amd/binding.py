@@ -285,23 +285,28 @@ def solar_apply_weights(In, W, Out, raise_on_error: bool = True) -> int:
 # Sequence operators.  Tensors of heads [B,N,heads,D] may be views with any strides that include/solar.h allows (a slice of
 # a packed projection, [B,heads,N,D] transposed); the calls go to the tensors' device and its current stream.
 
+# the current stream's handle without the Stream object around it, which takes as long to make as a launch
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _run(fn, tensors, args, raise_on_error: bool) -> int:
     """fn(*args, stream) on the device that all tensors are on."""
-    dev = None
+    dev = -1
     for t in tensors:
-        if t is None:
-            continue
-        if not t.is_cuda:
-            raise ValueError("tensors must be CUDA tensors")
-        if dev is None:
-            dev = t.device
-        elif t.device != dev:
-            raise ValueError("tensors must be on one device")
-    if dev.index == torch.cuda.current_device():
-        rc = fn(*args, torch.cuda.current_stream().cuda_stream)
+        if t is not None:
+            i = t.get_device()
+            if i < 0:
+                raise ValueError("tensors must be CUDA tensors")
+            if dev < 0:
+                dev = i
+            elif i != dev:
+                raise ValueError("tensors must be on one device")
+    stream = torch.cuda.current_stream(dev).cuda_stream if _raw_stream is None else _raw_stream(dev)
+    if dev == torch.cuda.current_device():
+        rc = fn(*args, stream)
     else:
         with torch.cuda.device(dev):
-            rc = fn(*args, torch.cuda.current_stream().cuda_stream)
+            rc = fn(*args, stream)
     if rc != SOLAR_OK and raise_on_error:
         raise SolarError(rc)
     return rc
@@ -311,25 +316,24 @@ def _like(name: str, t: Optional[torch.Tensor], dtype, shape):
     """data_ptr of a contiguous tensor of this type and shape, None for None."""
     if t is None:
         return None
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)}, got {t.dtype} "
-                         f"{tuple(t.shape)}")
+    if t.dtype != dtype or t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {shape}, got {t.dtype} {tuple(t.shape)}")
     return t.data_ptr()
 
 
-def _heads(name: str, t: torch.Tensor, dtype, shape):
-    """The three strides of a tensor of heads of this type and shape."""
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{name} must be a {dtype} tensor of shape {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
-    st = t.stride()
-    if st[3] != 1 and shape[3] > 1:
-        raise ValueError(f"the columns of {name} must be contiguous")
-    return st[:3]
-
-
-def _strides(*strides):
-    flat = [x for s in strides for x in s]
-    return (_i64 * len(flat))(*flat)
+def _heads(dtype, **tensors):
+    """The strides of tensors of heads, given as (tensor, shape), as the library takes them: None where all are contiguous."""
+    plain = True
+    for name, (t, shape) in tensors.items():
+        if t.dtype != dtype or t.shape != shape:
+            raise ValueError(f"{name} must be a {dtype} tensor of shape {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
+        if not t.is_contiguous():
+            plain = False
+            if t.stride(3) != 1 and shape[3] > 1:
+                raise ValueError(f"the columns of {name} must be contiguous")
+    if plain:
+        return None
+    return (_i64 * (3 * len(tensors)))(*[x for t, _ in tensors.values() for x in t.stride()[:3]])
 
 
 def _scratch(workspace: Optional[torch.Tensor]):
@@ -356,16 +360,14 @@ def solar_rotary(Q, K, freq, Qout, Kout, positions=None, lengths=None, layout: i
     """Rotates the first 2 * len(freq) columns of every head of Q [B,N,H,D] and K [B,N,Hkv,D] (K and Kout may be None)."""
     code = _dtype_code(Q)
     B, N, H, D = Q.shape
-    sq, sqo = _heads("Q", Q, Q.dtype, Q.shape), _heads("Qout", Qout, Q.dtype, Q.shape)
     if (K is None) != (Kout is None):
         raise ValueError("K and Kout go together")
-    Hkv, sk, sko = 0, sq, sqo
-    if K is not None:
-        Hkv = K.shape[2]
-        sk, sko = _heads("K", K, Q.dtype, (B, N, Hkv, D)), _heads("Kout", Kout, Q.dtype, (B, N, Hkv, D))
+    k, ko = (Q, Qout) if K is None else (K, Kout)
+    Hkv = k.shape[2]
+    st = _heads(Q.dtype, Q=(Q, Q.shape), K=(k, (B, N, Hkv, D)), Qout=(Qout, Q.shape), Kout=(ko, (B, N, Hkv, D)))
     args = (Q.data_ptr(), None if K is None else K.data_ptr(), _like("lengths", lengths, torch.int32, (B,)),
             _like("positions", positions, torch.int32, (B, N)), _like("freq", freq, torch.float64, (freq.numel(),)), B, N, H,
-            Hkv, D, 2 * freq.numel(), int(layout), int(inverse), float(amplitude), code, _strides(sq, sk, sqo, sko),
+            Hkv, D, 2 * freq.numel(), int(layout), int(inverse), float(amplitude), code, st,
             Qout.data_ptr(), None if Kout is None else Kout.data_ptr())
     return _run(_lib.solar_rotary, (Q, K, freq, Qout, Kout, positions, lengths), args, raise_on_error)
 
@@ -380,15 +382,16 @@ def solar_decay_attention(Q, K, V, log_decay, lengths, scale: float, O, state_in
     code = _dtype_code(K)
     B, N, Hkv, D = K.shape
     H = log_decay.numel()
-    sk, sv = _heads("K", K, K.dtype, K.shape), _heads("V", V, K.dtype, K.shape)
-    sq = so = (0, 0, 0)
-    if O is not None:
-        sq, so = _heads("Q", Q, K.dtype, (B, N, H, D)), _heads("O", O, K.dtype, (B, N, H, D))
+    shared = K.shape
+    if O is None:
+        st = _heads(K.dtype, Q=(K, shared), K=(K, shared), V=(V, shared), O=(K, shared))
+    else:
+        st = _heads(K.dtype, Q=(Q, (B, N, H, D)), K=(K, shared), V=(V, shared), O=(O, (B, N, H, D)))
     ws, wsb = _scratch(workspace)
     args = (None if O is None else Q.data_ptr(), K.data_ptr(), V.data_ptr(),
             _like("log_decay", log_decay, torch.float32, (H,)), _like("lengths", lengths, torch.int32, (B,)),
             _like("state_in", state_in, torch.float32, (B, H, D, D)), B, N, H, Hkv, D, float(scale), code,
-            _strides(sq, sk, sv, so), None if O is None else O.data_ptr(),
+            st, None if O is None else O.data_ptr(),
             _like("state_out", state_out, torch.float32, (B, H, D, D)), ws, wsb)
     return _run(_lib.solar_decay_attention,
                 (Q if O is not None else None, K, V, log_decay, lengths, O, state_in, state_out, workspace), args,
@@ -402,9 +405,8 @@ def solar_decay_attention_backward(Q, K, V, dO, log_decay, lengths, scale: float
     B, N, H, D = Q.shape
     Hkv = K.shape[2]
     shape, shared, dt = (B, N, H, D), (B, N, Hkv, D), Q.dtype
-    st = _strides(_heads("Q", Q, dt, shape), _heads("K", K, dt, shared), _heads("V", V, dt, shared),
-                  _heads("dO", dO, dt, shape), _heads("dQ", dQ, dt, shape), _heads("dK", dK, dt, shared),
-                  _heads("dV", dV, dt, shared))
+    st = _heads(dt, Q=(Q, shape), K=(K, shared), V=(V, shared), dO=(dO, shape), dQ=(dQ, shape), dK=(dK, shared),
+                dV=(dV, shared))
     ws, wsb = _scratch(workspace)
     states = (B, H, D, D)
     args = (Q.data_ptr(), K.data_ptr(), V.data_ptr(), dO.data_ptr(), _like("log_decay", log_decay, torch.float32, (H,)),
