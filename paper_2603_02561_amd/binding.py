@@ -542,3 +542,66 @@ class DeviceBatch:
     def dense(self, scale: float, O=None):
         return solar_dense_attention_ref(self.Q, self.X, self.lengths, scale,
                                          self.O if O is None else O, self.workspace)
+
+
+class SequenceMixer:
+    """A mixing layer over sequences in their order, from the sequence operators: rotary positions on queries and keys, linear
+    attention with a decay for each head, layer norm of every head's output.  Holds the buffers of one batch of B users with up
+    to N rows, the states that single tokens go on from, and with `training` the gradients.
+
+    log_decay [H] float, freq [rot/2] double, weight and bias [H,D] float: device tensors."""
+
+    def __init__(self, B: int, N: int, H: int, Hkv: int, D: int, dtype, log_decay, freq, weight, bias, eps: float = 1e-5,
+                 layout: int = SOLAR_ROTARY_HALF, training: bool = False):
+        dev = log_decay.device
+
+        def empty(*shape, dtype=torch.float32):
+            return torch.empty(shape, dtype=dtype, device=dev)
+
+        self.B, self.N, self.H, self.Hkv, self.D = B, N, H, Hkv, D
+        self.log_decay, self.freq, self.weight, self.bias, self.eps, self.layout = log_decay, freq, weight, bias, eps, layout
+        self.scale = D ** -0.5
+        self.Q, self.K = empty(B, N, H, D, dtype=dtype), empty(B, N, Hkv, D, dtype=dtype)
+        self.O, self.Y = empty(B, N, H, D, dtype=dtype), empty(B, N, H, D, dtype=dtype)
+        self.mean, self.rstd = empty(B * N, H), empty(B * N, H)
+        self.state = torch.zeros((B, H, D, D), dtype=torch.float32, device=dev)
+        self.positions = torch.zeros((B, 1), dtype=torch.int32, device=dev)
+        code = SOLAR_BF16 if dtype == torch.bfloat16 else SOLAR_F32
+        nbytes = solar_decay_workspace_bytes(B, N, H, Hkv, D, code, training)
+        if training:
+            nbytes = max(nbytes, solar_layer_norm_workspace_bytes(B * N, H, D))
+            self.dO = empty(B, N, H, D, dtype=dtype)
+            self.dQ, self.dK, self.dV = (empty(B, N, h, D, dtype=dtype) for h in (H, Hkv, Hkv))
+            self.dweight, self.dbias, self.dlog_decay = empty(H, D), empty(H, D), empty(H)
+        self.workspace = empty(max(nbytes, 256), dtype=torch.uint8)
+
+    def forward(self, Q, K, V, lengths=None):
+        """Y [B,N,H,D] for whole sequences, whose last states and lengths steps go on from."""
+        self._V, self._lengths = V, lengths
+        solar_rotary(Q, K, self.freq, self.Q, self.K, lengths=lengths, layout=self.layout)
+        solar_decay_attention(self.Q, self.K, V, self.log_decay, lengths, self.scale, self.O, None, self.state,
+                              self.workspace)
+        solar_layer_norm(self.O, self.weight, self.bias, self.eps, self.Y, self.mean, self.rstd)
+        if lengths is None:
+            self.positions.fill_(self.N)
+        else:
+            self.positions.copy_(lengths[:, None])
+        return self.Y
+
+    def step(self, Q, K, V):
+        """Y [B,1,H,D] for the next token of every user: Q [B,1,H,D], K and V [B,1,Hkv,D], K and Q rotated in place."""
+        solar_rotary(Q, K, self.freq, Q, K, positions=self.positions, layout=self.layout)
+        Y = torch.empty_like(Q)
+        solar_decay_attention(Q, K, V, self.log_decay, None, self.scale, Y, self.state, self.state)
+        solar_layer_norm(Y, self.weight, self.bias, self.eps, Y)
+        self.positions += 1
+        return Y
+
+    def backward(self, dY):
+        """Gradients of the last forward call: (dQ, dK, dV); dweight, dbias and dlog_decay are left in attributes."""
+        solar_layer_norm_backward(self.O, self.weight, self.mean, self.rstd, dY, self.dO, self.dweight, self.dbias,
+                                  self.workspace)
+        solar_decay_attention_backward(self.Q, self.K, self._V, self.dO, self.log_decay, self._lengths, self.scale, None, None,
+                                       self.dQ, self.dK, self.dV, None, self.dlog_decay, self.workspace)
+        solar_rotary(self.dQ, self.dK, self.freq, self.dQ, self.dK, lengths=self._lengths, layout=self.layout, inverse=True)
+        return self.dQ, self.dK, self.dV

@@ -75,12 +75,13 @@ __device__ __forceinline__ void split(v8f x, v8bf (&s)[T]) {
     }
 }
 
-// The same where neighbours must not meet: they are columns of an input.
-__device__ __forceinline__ void split_apart(v8f x, v8bf (&s)[3]) {
+// The same where neighbours must not meet (columns of an input), or x is kept: the instruction above overwrites it.
+template <int T>
+__device__ __forceinline__ void split_apart(v8f x, v8bf (&s)[T]) {
 #pragma unroll
-    for (int k = 0; k < 3; ++k) {
+    for (int k = 0; k < T; ++k) {
         s[k] = __builtin_convertvector(x, v8bf);
-        if (k < 2) x -= widen(s[k]);
+        if (k + 1 < T) x -= widen(s[k]);
     }
 }
 
@@ -231,7 +232,6 @@ decay_chunk_kernel(Walks ws) {
     using F = ChunkCfg<D, BF16, MOMENT>;
     constexpr int C = F::C, W = F::W, NB = F::NB, THREADS = F::kThreads, NT = F::NT, TP = F::TP, LP = F::LP;
     constexpr int NW = THREADS / 64, NS = D / W, NJ = D / 32, NC = C / 16, NK = C / 32, ES = BF16 ? 2 : 4;
-    constexpr bool kEarly = OUT && !MOMENT && BF16;
     constexpr int TM = MOMENT ? 3 : 1, MB = MOMENT ? NB : 1, MJ = MOMENT ? NJ : 1;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     __bf16* const ki = reinterpret_cast<__bf16*>(lds);                  // [NT][C][D]
@@ -279,7 +279,9 @@ decay_chunk_kernel(Walks ws) {
         }
     }
 
-    // S[j][nb][a]: rows 32 j + 8 g4 + 4 a + (0..3), column mycol + 16 nb + c16 for lane 16 g4 + c16; T: its derivative
+    // S[j][nb][a]: rows 32 j + 8 g4 + 4 a + (0..3), column mycol + column(c16, nb) for lane 16 g4 + c16; T: its derivative.  With
+    // two tiles their columns alternate in fours, so that a lane's entries of O^T are eight in a row.
+    auto column = [](int c16, int nb) { return NB == 2 ? 8 * (c16 >> 2) + 4 * nb + (c16 & 3) : 16 * nb + c16; };
     v4f S[NJ][NB][2], T[MJ][MB][2];
     const size_t state_at = ((size_t)b * w.H + h) * D * D;
     const size_t part_at = ((size_t)b * w.H + h) * (w.nparts - 1) * D * D;
@@ -294,7 +296,7 @@ decay_chunk_kernel(Walks ws) {
                 for (int a = 0; a < 2; ++a)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const int r = 32 * j + 8 * g4 + 4 * a + i, col = mycol + 16 * nb + c16;
+                        const int r = 32 * j + 8 * g4 + 4 * a + i, col = mycol + column(c16, nb);
                         f((uint32_t)(r * D + col), (uint32_t)(col * D + r), j, nb, a, i);
                     }
     };
@@ -328,13 +330,14 @@ decay_chunk_kernel(Walks ws) {
     }
 
     // places in the images: chunk g4 of row c16; this lane's four elements of row 8 g4 + c16 / 4 for K^T (columns
-    // 8 (c16 % 4) ..) and for V (this wave's columns, 4 (c16 % 4) ..)
+    // 8 (c16 % 4) ..) and for V (this wave's columns, 8 (c16 % 4) .. or with one tile 4 (c16 % 4) ..)
     uint32_t row_at, kt_at, v_at;
     {
         const int c16 = tid & 15, g4 = tid >> 4 & 3, trow = 8 * g4 + (c16 >> 2);
         row_at = c16 * D + ((g4 ^ swizzle<D>(c16)) << 3);
         kt_at = trow * D + (((c16 & 3) ^ swizzle<D>(trow)) << 3);
-        v_at = trow * W + (((2 * NB * wave + (c16 >> 1 & 1)) ^ swizzle<W>(trow)) << 3) + 4 * (c16 & 1);
+        v_at = NB == 2 ? trow * W + (((4 * wave + (c16 & 3)) ^ swizzle<W>(trow)) << 3)
+                       : trow * W + (((2 * wave + (c16 >> 1 & 1)) ^ swizzle<W>(trow)) << 3) + 4 * (c16 & 1);
     }
     const float gfull = expm1f(lg * (float)C);
     double z = 0.;          // terms of either sign over thousands of rows
@@ -360,7 +363,7 @@ decay_chunk_kernel(Walks ws) {
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-                for (int k = 0; k < NT; ++k) v[nb][k] = lds_turned<W>(vi + (k * C + 32 * kk) * W, v_at ^ (nb << 4));
+                for (int k = 0; k < NT; ++k) v[nb][k] = lds_turned<W>(vi + (k * C + 32 * kk) * W + 4 * nb, v_at);
         };
         v4f O[NB][NC], R[MB][MOMENT ? NC : 1];
         // O = Q S times g^(i+pre), R its derivative; the rows of Q are read a step ahead, or not (for fewer registers)
@@ -391,7 +394,7 @@ decay_chunk_kernel(Walks ws) {
                     v8f x;
 #pragma unroll
                     for (int e = 0; e < 8; ++e) x[e] = S[j][nb][e / 4][e % 4];
-                    split<TP>(x, s[nb]);
+                    split_apart(x, s[nb]);
                 }
                 products(s, q[j & A], O);
                 if constexpr (MOMENT) {
@@ -401,7 +404,7 @@ decay_chunk_kernel(Walks ws) {
                         v8f x;
 #pragma unroll
                         for (int e = 0; e < 8; ++e) x[e] = T[j][nb][e / 4][e % 4];
-                        split<3>(x, m[nb]);
+                        split_apart(x, m[nb]);
                     }
                     products(m, q[j & A], R);
                 }
@@ -475,12 +478,8 @@ decay_chunk_kernel(Walks ws) {
                     put(x, mi + to, Number<3>());
                 }
             }
-            from_state(Number<1>());
+            from_state(Number<MOMENT ? 0 : 1>());
             __syncthreads();
-            if (kEarly) {
-                fk.load(kr, done + C, count);
-                fq.load(qr, done + C, count);
-            }
 
             // tiles 2 t2 and 2 t2 + 1 of the columns of P's images, against 32 kk rows of V
             auto read_p = [&](const __bf16* img, int kk, int t2, auto& p) __attribute__((always_inline)) {
@@ -582,35 +581,38 @@ decay_chunk_kernel(Walks ws) {
             for (int t = 0; t < NC; ++t)
                 if (16 * t + c16 < cnt) {
                     const bool o_float = !BF16 || w.o_float;
-                    const uint32_t at = outr.off(16 * t + c16) + (mycol + 4 * g4) * (o_float ? 4 : 2);
+                    const int col = mycol + 4 * NB * g4;
+                    char* const p = const_cast<char*>(outp) + (outr.off(16 * t + c16) + col * (o_float ? 4 : 2));
+                    if (o_float) {
 #pragma unroll
-                    for (int nb = 0; nb < NB; ++nb) {
-                        char* p = const_cast<char*>(outp + at) + nb * (o_float ? 64 : 32);
-                        if (o_float) *reinterpret_cast<v4f*>(p) = O[nb][t];
-                        else *reinterpret_cast<v4bf*>(p) = __builtin_convertvector(O[nb][t], v4bf);
-                        if constexpr (MODE == kMoment) {
-                            const char* q = gradp + (gradr.off(16 * t + c16) + (mycol + 16 * nb + 4 * g4) * ES);
-                            v4f d;
-                            if constexpr (BF16) {
-                                const uint2 u = *reinterpret_cast<const uint2*>(q);
-                                d = v4f{bf16_lo(u.x), bf16_hi(u.x), bf16_lo(u.y), bf16_hi(u.y)};
-                            } else {
-                                d = *reinterpret_cast<const v4f*>(q);
-                            }
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) zc = fmaf(R[nb][t][e], d[e], zc);
+                        for (int nb = 0; nb < NB; ++nb) *reinterpret_cast<v4f*>(p + 16 * nb) = O[nb][t];
+                    } else if constexpr (NB == 2) {
+                        const v8f x = __builtin_shufflevector(O[0][t], O[NB - 1][t], 0, 1, 2, 3, 4, 5, 6, 7);
+                        *reinterpret_cast<v8bf*>(p) = __builtin_convertvector(x, v8bf);
+                    } else {
+                        *reinterpret_cast<v4bf*>(p) = __builtin_convertvector(O[0][t], v4bf);
+                    }
+                    if constexpr (MODE == kMoment) {
+                        static_assert(!MOMENT || NB == 1, "");
+                        const char* q = gradp + (gradr.off(16 * t + c16) + col * ES);
+                        v4f d;
+                        if constexpr (BF16) {
+                            const uint2 u = *reinterpret_cast<const uint2*>(q);
+                            d = v4f{bf16_lo(u.x), bf16_hi(u.x), bf16_lo(u.y), bf16_hi(u.y)};
+                        } else {
+                            d = *reinterpret_cast<const v4f*>(q);
                         }
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) zc = fmaf(R[0][t][e], d[e], zc);
                     }
                 }
             if constexpr (MODE == kMoment) z += zc;
         }
 
         // the next rows are on their way while S is updated, where registers are free for them
-        if (!kEarly) {
-            fk.load(kr, done + C, count);
-            if constexpr (OUT) fq.load(qr, done + C, count);
-        }
+        fk.load(kr, done + C, count);
         fv.load(vr, done + C, count);
+        if constexpr (OUT) fq.load(qr, done + C, count);
 
         // S <- g^cnt S + K^T diag(g^(cnt-pre-j)) V, and T <- g^cnt (T + cnt S) + ... with the weights' derivative
         const float gc = cnt == C ? gfull : expm1f(lg * (float)cnt);

@@ -57,8 +57,11 @@ struct Walks {
 };
 
 // decay.hip
-// A forward walk row by row, for a few rows (N <= kDecayRows); nparts is not looked at.
-constexpr int kDecayRows = 8;
+// A forward walk row by row, for a few rows (N <= kDecayRows); nparts is not looked at.  Every row costs it a sum across the
+// workgroup, the chunked form takes up to 32 or 64 rows at the price of one: 4 rows of 1024 states take 15.3 against 16.2 us at
+// D = 64, 32.5 against 37.4 at 128, 8 rows 22.2 against 16.1 and 44.5 against 37.4 (bf16; four states 5.6 against 6.6 and 8.7
+// against 6.6 at D = 64).
+constexpr int kDecayRows = 4;
 hipError_t launch_decay_rows(const Walk& w, hipStream_t stream);
 // dlog[h] = the sum of moments [B][H][slices] over users and slices
 hipError_t launch_moment_sum(const double* moments, int B, int H, int slices, float* dlog, hipStream_t stream);
