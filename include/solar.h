@@ -400,7 +400,7 @@ solar_status solar_decay_attention_backward(const void* Q, const void* K, const 
  *   In      in [rows, groups, d] of type t_in         weight, bias  in [groups, d] float, each may be NULL (1, 0)
  *   Out     out [rows, groups, d] of type t_out; may be In itself if the two types are the same
  *   mean, rstd  out [rows, groups] float, for the gradient; each may be NULL
- * Supported: d <= 16384 (any), groups <= 2^20, groups * d <= 2^28, rows * groups < 2^31.
+ * Supported: d <= 16384 (any), groups <= 2^20, groups * d <= 2^26, rows * groups < 2^31.
  */
 solar_status solar_layer_norm(const void* In, const float* weight, const float* bias, int rows, int groups, int d,
                               float eps, solar_dtype t_in, solar_dtype t_out, void* Out, float* mean, float* rstd,

@@ -58,16 +58,15 @@ solar_status check_decay(int B, int N, int H, int Hkv, int D, float scale, solar
         return SOLAR_ERR_INVALID_ARG;
     if (D != 64 && D != 128 && D != 256) return SOLAR_ERR_UNSUPPORTED;
     if (N > 1 << 30) return SOLAR_ERR_UNSUPPORTED;
-    // workgroups of the row form and of the chunked form, which go by users, heads and slices, and no part is cut below 512 rows
-    const int64_t slices = D / 32, parts = 1 + N / 512;
-    if ((int64_t)B * H * slices > kMaxBlocks / 2 || (int64_t)B * H * slices > kMaxBlocks / 2 * 512 / parts)
-        return SOLAR_ERR_UNSUPPORTED;
+    // Workgroups of the row form go by users, heads and slices; those of the chunked form are fewer, but twice the size and for two
+    // walks at once, and parts are only cut where there are less than 512.
+    if ((int64_t)B * H * (D / 32) > kMaxBlocks / 4) return SOLAR_ERR_UNSUPPORTED;
     return SOLAR_OK;
 }
 
 struct DecayCarve {
     DecayParts cut;
-    float *parts, *part_moments;    // [B,H,parts-1,D,D]
+    float *parts, *part_moments;    // [B,H,parts,D,D], none for one part
     float *dk, *dv;                 // [B,N,H,D] of every head, where heads share K and V
     double* moments;                // [B,H,parts,slices]
     size_t total;
@@ -83,7 +82,7 @@ DecayCarve carve_decay(void* ws, int B, int N, int H, int Hkv, int D, bool backw
     };
     if (!backward && N <= kDecayRows) return c;
     c.cut = decay_parts(B, N, H, D, backward ? 2 : 1);
-    const size_t states = (size_t)B * H * (c.cut.parts - 1) * D * D;
+    const size_t states = c.cut.parts > 1 ? (size_t)B * H * c.cut.parts * D * D : 0;
     c.parts = part(states);
     if (backward) {
         const size_t shared = H != Hkv ? (size_t)B * N * H * D : 0;
@@ -289,7 +288,7 @@ solar_status solar_decay_attention_backward(const void* Q, const void* K, const 
 
 static solar_status check_norm(int rows, int groups, int d) {
     if (rows <= 0 || groups <= 0 || d <= 0) return SOLAR_ERR_INVALID_ARG;
-    if (d > kNormMaxD || groups > 1 << 20 || (int64_t)groups * d > (1 << 28) || (int64_t)rows * groups > INT_MAX) return SOLAR_ERR_UNSUPPORTED;
+    if (d > kNormMaxD || groups > 1 << 20 || (int64_t)groups * d > (1 << 26) || (int64_t)rows * groups > INT_MAX) return SOLAR_ERR_UNSUPPORTED;
     return SOLAR_OK;
 }
 

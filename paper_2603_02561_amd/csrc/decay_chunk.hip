@@ -218,7 +218,7 @@ __device__ __forceinline__ void update(const v8bf (&k)[A][TA], const v8bf (&v)[N
                     for (int a = 0; a < A; ++a) c[nb][a] = mfma(k[a][i], v[nb][sum - i], c[nb][a]);
 }
 
-// kOut: outputs; kState: the state behind each part but the last, from a zero state, into w.parts; kMoment: outputs, and their
+// kOut: outputs; kState: the state behind each part but the last, from a zero state, into its place in w.parts; kMoment: outputs, and their
 // derivative by log g summed against w.grad; kMomentState: kState, and the derivative of these states; kLast: the state behind
 // the last part, where nobody wants outputs.
 enum { kOut, kState, kMoment, kMomentState, kLast };
@@ -284,7 +284,7 @@ decay_chunk_kernel(Walks ws) {
     auto column = [](int c16, int nb) { return NB == 2 ? 8 * (c16 >> 2) + 4 * nb + (c16 & 3) : 16 * nb + c16; };
     v4f S[NJ][NB][2], T[MJ][MB][2];
     const size_t state_at = ((size_t)b * w.H + h) * D * D;
-    const size_t part_at = ((size_t)b * w.H + h) * (w.nparts - 1) * D * D;
+    const size_t part_at = (((size_t)b * w.H + h) * w.nparts + order) * D * D;
     // f(the place of an entry in a state, the same in a transposed one, j, nb, a, i)
     auto entries = [&](auto f) __attribute__((always_inline)) {
         const int c16 = tid & 15, g4 = tid >> 4 & 3;
@@ -301,13 +301,13 @@ decay_chunk_kernel(Walks ws) {
                     }
     };
     {
-        const bool own = order > 0 && !STATES;          // starts where the part before ends
-        const float* start = STATES ? nullptr : own ? w.parts + part_at + (size_t)(order - 1) * D * D
-                                                    : w.state_in ? w.state_in + state_at : nullptr;
-        const bool turned = own ? w.parts_turned : w.in_turned;
+        // where there are parts all start from w.parts, the first too: state_out may be state_in
+        const bool cut = w.nparts > 1;
+        const float* start = STATES ? nullptr : cut ? w.parts + part_at : w.state_in ? w.state_in + state_at : nullptr;
+        const bool turned = cut ? w.parts_turned : w.in_turned;
         entries([&](uint32_t at, uint32_t across, int j, int nb, int a, int i) {
             S[j][nb][a][i] = start ? start[turned ? across : at] : 0.f;
-            if constexpr (MOMENT) T[j][nb][a][i] = own ? w.part_moments[part_at + (size_t)(order - 1) * D * D + at] : 0.f;
+            if constexpr (MOMENT) T[j][nb][a][i] = cut && !STATES ? w.part_moments[part_at + at] : 0.f;
         });
     }
 
@@ -672,16 +672,16 @@ decay_chunk_kernel(Walks ws) {
     if constexpr (OUT) {
         // rows of this part that are not valid
         const int es = BF16 && !w.o_float ? 2 : 4, vecs = W * es / 16;
-        for (int i = tid; i < (rows - count) * vecs; i += THREADS) {
+        for (int64_t i = tid; i < (int64_t)(rows - count) * vecs; i += THREADS) {
             char* p = row_of(w.o, b, row0 + count + i / vecs, h) + (size_t)col0 * es + i % vecs * 16;
             *reinterpret_cast<v4u*>(p) = v4u{0u, 0u, 0u, 0u};
         }
     }
-    float* to = STATES ? w.parts + part_at + (size_t)order * D * D : order == w.nparts - 1 && w.state_out ? w.state_out + state_at : nullptr;
+    float* to = STATES ? w.parts + part_at : order == w.nparts - 1 && w.state_out ? w.state_out + state_at : nullptr;
     if (to) entries([&](uint32_t at, uint32_t, int j, int nb, int a, int i) { to[at] = S[j][nb][a][i]; });
     if constexpr (MODE == kMomentState)
         entries([&](uint32_t at, uint32_t, int j, int nb, int a, int i) {
-            w.part_moments[part_at + (size_t)order * D * D + at] = T[j][nb][a][i];
+            w.part_moments[part_at + at] = T[j][nb][a][i];
         });
     if constexpr (MODE == kMoment) {
         if (order == w.nparts - 1 && w.grad_state)
@@ -701,8 +701,8 @@ decay_chunk_kernel(Walks ws) {
     }
 }
 
-// parts[o] holds the state behind part o of the walk from a zero state; it becomes the state behind parts 0 .. o from
-// state_in, which is the start of part o + 1.
+// parts[o] holds the state behind part o of the walk from a zero state (nothing yet for the last part); it becomes the state that
+// part o starts from.
 template <bool MOMENT>
 __global__ __launch_bounds__(kJoinThreads) void join_parts_kernel(Walk w) {
     const int DD = w.D * w.D;
@@ -713,21 +713,24 @@ __global__ __launch_bounds__(kJoinThreads) void join_parts_kernel(Walk w) {
     const size_t bh = (size_t)b * w.H + h;
     float s = 0.f, t = 0.f;
     if (w.state_in) s = w.state_in[bh * DD + (w.in_turned ? (e % w.D) * w.D + e / w.D : e)];
-    float* p = w.parts + bh * (w.nparts - 1) * DD + e;
-    float* pm = MOMENT ? w.part_moments + bh * (w.nparts - 1) * DD + e : nullptr;
+    float* p = w.parts + bh * w.nparts * DD + e;
+    float* pm = MOMENT ? w.part_moments + bh * w.nparts * DD + e : nullptr;
     for (int o = 0; o + 1 < w.nparts; ++o) {
         const int part = w.reverse ? w.nparts - 1 - o : o, row0 = part * w.part_rows;
         const int rows = w.N - row0 < w.part_rows ? w.N - row0 : w.part_rows;
         const int count = len - row0 < 0 ? 0 : (len - row0 < rows ? len - row0 : rows);
         const float g = expm1f(lg * (float)count), gc = count ? g : 0.f;      // log g may be -infinity
         if constexpr (MOMENT) {
-            const float x = fmaf((float)count, s, t);
-            t = fmaf(x, gc, x) + pm[(size_t)o * DD];
+            const float add = pm[(size_t)o * DD], x = fmaf((float)count, s, t);
             pm[(size_t)o * DD] = t;
+            t = fmaf(x, gc, x) + add;
         }
-        s = fmaf(s, gc, s) + p[(size_t)o * DD];
+        const float add = p[(size_t)o * DD];
         p[(size_t)o * DD] = s;
+        s = fmaf(s, gc, s) + add;
     }
+    p[(size_t)(w.nparts - 1) * DD] = s;
+    if constexpr (MOMENT) pm[(size_t)(w.nparts - 1) * DD] = t;
 }
 
 template <int D, bool BF16, int MODE>

@@ -23,48 +23,48 @@ struct Elem<true> {
     using type = __bf16;
 };
 
-typedef __bf16 v4bf __attribute__((ext_vector_type(4)));
-
-// eight consecutive elements at p
-template <bool BF16>
+// Eight consecutive elements at p; ALIGNED: at a multiple of 16 bytes, else wherever an element may be (the memory takes that in
+// one access too).
+template <bool BF16, bool ALIGNED>
 __device__ __forceinline__ void load8(const char* p, float (&x)[8]) {
-    if constexpr (BF16) {
-        const v4u u = *reinterpret_cast<const v4u*>(p);
+    constexpr int V = BF16 ? 1 : 2;
+    v4u u[V];
+    if constexpr (ALIGNED) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            x[2 * i] = bf16_lo(u[i]);
-            x[2 * i + 1] = bf16_hi(u[i]);
-        }
+        for (int j = 0; j < V; ++j) u[j] = reinterpret_cast<const v4u*>(p)[j];
     } else {
+        __builtin_memcpy(u, __builtin_assume_aligned(p, BF16 ? 2 : 4), sizeof(u));
+    }
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const v4f u = reinterpret_cast<const v4f*>(p)[j];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) x[4 * j + i] = u[i];
-        }
+    for (int i = 0; i < 8; ++i) {
+        if constexpr (BF16) x[i] = i & 1 ? bf16_hi(u[0][i / 2]) : bf16_lo(u[0][i / 2]);
+        else x[i] = __uint_as_float(u[i / 4][i % 4]);
     }
 }
 
-template <bool BF16>
+template <bool BF16, bool ALIGNED>
 __device__ __forceinline__ void store8(char* p, const float (&x)[8]) {
     if constexpr (BF16) {
         v8bf u;
 #pragma unroll
         for (int i = 0; i < 8; ++i) u[i] = (__bf16)x[i];
-        *reinterpret_cast<v8bf*>(p) = u;
+        if constexpr (ALIGNED) *reinterpret_cast<v8bf*>(p) = u;
+        else __builtin_memcpy(__builtin_assume_aligned(p, 2), &u, sizeof(u));
     } else {
+        v4f u[2] = {{x[0], x[1], x[2], x[3]}, {x[4], x[5], x[6], x[7]}};
+        if constexpr (ALIGNED) {
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            v4f u = {x[4 * j], x[4 * j + 1], x[4 * j + 2], x[4 * j + 3]};
-            reinterpret_cast<v4f*>(p)[j] = u;
+            for (int j = 0; j < 2; ++j) reinterpret_cast<v4f*>(p)[j] = u[j];
+        } else {
+            __builtin_memcpy(__builtin_assume_aligned(p, 4), u, sizeof(u));
         }
     }
 }
 
-// VEC: whole vectors of eight columns lie in one half (or one run of pairs) of the rotated columns.  A unit is then two
-// vectors of eight (half layout), one of them (interleaved), or one vector of columns that are copied; otherwise it is one
-// pair, or one copied column.
-template <bool BF16, bool INTERLEAVED, bool VEC>
+// A head is cut into units, one for a thread at a time: eight pairs (half layout; their second columns start on a vector where
+// EVEN) or four (interleaved), then the pairs that are left over, then the columns to copy: up to the next vector one by one,
+// then by vectors.  Every unit reads its columns before it writes them, and no two share one, so a call may be in place.
+template <bool BF16, bool INTERLEAVED, bool EVEN>
 __global__ __launch_bounds__(kThreads) void rotary_kernel(Rotary r, int tokens, bool copy) {
     using E = typename Elem<BF16>::type;
     constexpr int ES = BF16 ? 2 : 4;
@@ -83,13 +83,15 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(Rotary r, int tokens, 
         turn[i] = make_float2(r.amplitude * c, r.inverse ? -r.amplitude * s : r.amplitude * s);
     }
     __syncthreads();
-    const int rot_units = VEC ? (INTERLEAVED ? r.rot / 8 : r.rot / 16) : pairs;
-    const int copy_units = VEC ? (r.D - r.rot) / 8 : r.D - r.rot;
-    const int units = rot_units + copy_units, heads = r.heads[0] + r.heads[1];
+    const int whole = INTERLEAVED ? r.rot / 8 : pairs / 8;              // units of vectors
+    const int odd = INTERLEAVED ? r.rot % 8 / 2 : pairs % 8;            // pairs left over
+    const int lone = (8 - r.rot % 8) % 8;                               // columns up to the next vector
+    const int units = whole + odd + lone + (r.D - r.rot - lone) / 8, heads = r.heads[0] + r.heads[1];
     const int per_token = units * heads;
     for (int i = threadIdx.x; i < count * per_token; i += kThreads) {
         const int tok = i / per_token, in_tok = i - tok * per_token;
-        const int hh = in_tok / units, u = in_tok - hh * units;
+        const int hh = in_tok / units;
+        int u = in_tok - hh * units;
         const int64_t bn = first + tok;
         const int b = (int)(bn / r.N), n = (int)(bn - (int64_t)b * r.N);
         const int which = hh >= r.heads[0];
@@ -98,54 +100,54 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(Rotary r, int tokens, 
         char* out = row_of(r.out[which], b, n, h);
         const bool valid = n < user_len(r.lengths, b, r.N);
         const float2* cs = turn + tok * pairs;
-        if (u >= rot_units) {
-            const int c = r.rot + (u - rot_units) * (VEC ? 8 : 1);
-            if constexpr (VEC) {
-                if (valid && !copy) continue;
+        if (u < whole) {
+            float x[8], y[8];
+            if constexpr (INTERLEAVED) {
+                load8<BF16, true>(in + 8 * u * ES, x);
 #pragma unroll
-                for (int j = 0; j < ES / 2; ++j) {
-                    const v4u zero = {0u, 0u, 0u, 0u};
-                    reinterpret_cast<v4u*>(out + c * ES)[j] = valid ? reinterpret_cast<const v4u*>(in + c * ES)[j] : zero;
+                for (int j = 0; j < 4; ++j) {
+                    const float2 t = cs[4 * u + j];
+                    y[2 * j] = valid ? x[2 * j] * t.x - x[2 * j + 1] * t.y : 0.f;
+                    y[2 * j + 1] = valid ? x[2 * j + 1] * t.x + x[2 * j] * t.y : 0.f;
                 }
+                store8<BF16, true>(out + 8 * u * ES, y);
             } else {
-                if (valid && !copy) continue;
-                reinterpret_cast<E*>(out)[c] = valid ? reinterpret_cast<const E*>(in)[c] : (E)0.f;
+                load8<BF16, true>(in + 8 * u * ES, x);
+                load8<BF16, EVEN>(in + (pairs + 8 * u) * ES, y);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float2 t = cs[8 * u + j];
+                    const float a = x[j], d = y[j];
+                    x[j] = valid ? a * t.x - d * t.y : 0.f;
+                    y[j] = valid ? d * t.x + a * t.y : 0.f;
+                }
+                store8<BF16, true>(out + 8 * u * ES, x);
+                store8<BF16, EVEN>(out + (pairs + 8 * u) * ES, y);
             }
-        } else if constexpr (!VEC) {
-            const int ca = INTERLEAVED ? 2 * u : u, cb = INTERLEAVED ? 2 * u + 1 : u + pairs;
+        } else if (u -= whole; u < odd) {
+            const int p = (INTERLEAVED ? 4 : 8) * whole + u;
+            const int ca = INTERLEAVED ? 2 * p : p, cb = INTERLEAVED ? 2 * p + 1 : p + pairs;
             float a = 0.f, d = 0.f;
             if (valid) {
                 a = (float)reinterpret_cast<const E*>(in)[ca];
                 d = (float)reinterpret_cast<const E*>(in)[cb];
-                const float x = a * cs[u].x - d * cs[u].y;
-                d = d * cs[u].x + a * cs[u].y;
+                const float x = a * cs[p].x - d * cs[p].y;
+                d = d * cs[p].x + a * cs[p].y;
                 a = x;
             }
             reinterpret_cast<E*>(out)[ca] = (E)a;
             reinterpret_cast<E*>(out)[cb] = (E)d;
-        } else if constexpr (INTERLEAVED) {
-            float x[8], y[8];
-            load8<BF16>(in + 8 * u * ES, x);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float2 t = cs[4 * u + j];
-                y[2 * j] = valid ? x[2 * j] * t.x - x[2 * j + 1] * t.y : 0.f;
-                y[2 * j + 1] = valid ? x[2 * j + 1] * t.x + x[2 * j] * t.y : 0.f;
-            }
-            store8<BF16>(out + 8 * u * ES, y);
+        } else if (valid && !copy) {
+            continue;
+        } else if (u -= odd; u < lone) {
+            reinterpret_cast<E*>(out)[r.rot + u] = valid ? reinterpret_cast<const E*>(in)[r.rot + u] : (E)0.f;
         } else {
-            float x[8], y[8];
-            load8<BF16>(in + 8 * u * ES, x);
-            load8<BF16>(in + (pairs + 8 * u) * ES, y);
+            const int c = r.rot + lone + (u - lone) * 8;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const float2 t = cs[8 * u + j];
-                const float a = x[j], d = y[j];
-                x[j] = valid ? a * t.x - d * t.y : 0.f;
-                y[j] = valid ? d * t.x + a * t.y : 0.f;
+            for (int j = 0; j < ES / 2; ++j) {
+                const v4u zero = {0u, 0u, 0u, 0u};
+                reinterpret_cast<v4u*>(out + c * ES)[j] = valid ? reinterpret_cast<const v4u*>(in + c * ES)[j] : zero;
             }
-            store8<BF16>(out + 8 * u * ES, x);
-            store8<BF16>(out + (pairs + 8 * u) * ES, y);
         }
     }
 }
@@ -159,15 +161,20 @@ hipError_t launch_rotary(const Rotary& r, hipStream_t stream) {
     const int64_t all = (int64_t)r.B * r.N;
     const dim3 grid((unsigned)((all + tokens - 1) / tokens)), block(kThreads);
     const size_t lds = sizeof(float2) * tokens * pairs;
-    const bool vec = r.interleaved ? r.rot % 8 == 0 : r.rot % 16 == 0;
-    const bool copy = r.in[0].data != r.out[0].data || (r.heads[1] && r.in[1].data != r.out[1].data);
+    const bool even = r.interleaved || r.rot % 16 == 0;
+    auto same = [](const Heads& x, const Heads& y) {
+        return x.data == y.data && x.s.batch == y.s.batch && x.s.row == y.s.row && x.s.head == y.s.head;
+    };
+    const bool copy = !same(r.in[0], r.out[0]) || (r.heads[1] && !same(r.in[1], r.out[1]));
 #define SOLAR_ROTARY(BF, IL, V) hipLaunchKernelGGL((rotary_kernel<BF, IL, V>), grid, block, lds, stream, r, tokens, copy)
     if (r.bf16) {
-        if (r.interleaved) { if (vec) SOLAR_ROTARY(true, true, true); else SOLAR_ROTARY(true, true, false); }
-        else { if (vec) SOLAR_ROTARY(true, false, true); else SOLAR_ROTARY(true, false, false); }
+        if (r.interleaved) SOLAR_ROTARY(true, true, true);
+        else if (even) SOLAR_ROTARY(true, false, true);
+        else SOLAR_ROTARY(true, false, false);
     } else {
-        if (r.interleaved) { if (vec) SOLAR_ROTARY(false, true, true); else SOLAR_ROTARY(false, true, false); }
-        else { if (vec) SOLAR_ROTARY(false, false, true); else SOLAR_ROTARY(false, false, false); }
+        if (r.interleaved) SOLAR_ROTARY(false, true, true);
+        else if (even) SOLAR_ROTARY(false, false, true);
+        else SOLAR_ROTARY(false, false, false);
     }
 #undef SOLAR_ROTARY
     return hipGetLastError();

@@ -37,7 +37,7 @@ struct Walk {
     bool reverse, in_turned;        // in_turned: state_in is read transposed
     bool bf16, o_float;             // o_float: o is float whatever the inputs are
     // the sequence is cut into nparts parts of part_rows rows (a multiple of 64); parts and part_moments are
-    // [B,H,nparts-1,D,D] work arrays, not used where nparts is 1
+    // [B,H,nparts,D,D] work arrays, not used where nparts is 1
     int nparts, part_rows;
     float *parts, *part_moments;
     bool parts_turned;              // parts hold the states of this walk transposed

@@ -384,3 +384,48 @@ def test_against_differences_of_the_operator(lib):
         setattr(p, name, x)
         # A grows with |x + d|, by less than threefold for standard normal values on both sides
         assert abs((after - before) - (g.double().cpu() * moved).sum()) < 4 * bound, name
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("N,D", [(700, 64), (2000, 128), (900, 256), (20, 128)])
+def test_state_in_place_over_parts(lib, N, D, dtype):
+    """The last state may go where the first came from, also where the sequence is cut into parts and the last ones are empty."""
+    p = Problem(3, N, 2, 1, D, dtype, lengths=[N, 10, 0], state=True, seed=N)
+    o, s = forward(lib, p)
+    first = p.state.cuda()
+    p.state = first
+    o2, s2 = forward(lib, p, state_out=first)
+    assert s2 is first and torch.equal(o, o2) and torch.equal(s, s2)
+
+
+def test_shared_rows_and_far_strides(lib):
+    """One K for all users (a stride of zero), and rows far apart."""
+    p = Problem(3, 100, 2, 2, 64, "bf16", seed=3)
+    p.k = p.k[:1].expand(3, -1, -1, -1).contiguous()
+    o, s = forward(lib, p)
+    k = p.k[:1].cuda().expand(3, -1, -1, -1)
+    wide = torch.zeros(3, 100, 2, 1 << 12, dtype=p.dt, device="cuda")
+    wide[..., :64] = p.v.cuda()
+    o2, s2 = forward(lib, p, k=k, v=wide[..., :64])
+    assert torch.equal(o, o2) and torch.equal(s, s2)
+
+
+def test_another_device_is_not_mixed_in(lib):
+    p = Problem(1, 5, 1, 1, 64, "f32")
+    with pytest.raises(ValueError):
+        forward(lib, p, k=p.k)
+
+
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_gradients_after_a_nan_leave_later_rows(lib, dtype, D):
+    """dK and dV come from the rows behind: a NaN in the gradient of row t reaches those of rows up to t alone, and dQ of row t alone."""
+    p = Problem(1, 200, 1, 1, D, dtype, seed=6, backward=True)
+    want = backward(lib, p)
+    p.do[0, 100, 0, 3] = float("nan")
+    got = backward(lib, p)
+    for i in (1, 2):
+        assert torch.equal(got[i][0, 101:], want[i][0, 101:])
+        assert not torch.isfinite(got[i][0, 100]).all()
+    keep = torch.arange(200) != 100
+    assert torch.equal(got[0].cpu()[0, keep], want[0].cpu()[0, keep]) and torch.isnan(got[0][0, 100]).any()

@@ -44,7 +44,7 @@ def check(x, got, pos, freq, interleaved, inverse=False, amplitude=1.0, lengths=
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("interleaved", [False, True])
 @pytest.mark.parametrize("D,rot", [(64, 64), (128, 64), (128, 32), (64, 2), (64, 20), (64, 24), (256, 256), (8, 8), (24, 18), (512, 512),
-                                   (72, 48)])
+                                   (72, 48), (256, 152), (256, 250), (64, 62), (16, 14)])
 def test_sizes(lib, D, rot, interleaved, dtype):
     q, k = inputs(3, 11, 5, 2, D, dtype, seed=D + rot)
     freq = lib.solar_rotary_frequencies(rot)
