@@ -63,7 +63,7 @@ __device__ __forceinline__ void store8(char* p, const float (&x)[8]) {
 
 // A head is cut into units, one for a thread at a time: eight pairs (half layout; their second columns start on a vector where
 // EVEN) or four (interleaved), then the pairs that are left over, then the columns to copy: up to the next vector one by one,
-// then by vectors.  Every unit reads its columns before it writes them, and no two share one, so a call may be in place.
+// then by vectors.  Every unit reads its columns before it writes them, and no two share a column, so a call may be in place.
 template <bool BF16, bool INTERLEAVED, bool EVEN>
 __global__ __launch_bounds__(kThreads) void rotary_kernel(Rotary r, int tokens, bool copy) {
     using E = typename Elem<BF16>::type;
@@ -86,67 +86,85 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(Rotary r, int tokens, 
     const int whole = INTERLEAVED ? r.rot / 8 : pairs / 8;              // units of vectors
     const int odd = INTERLEAVED ? r.rot % 8 / 2 : pairs % 8;            // pairs left over
     const int lone = (8 - r.rot % 8) % 8;                               // columns up to the next vector
-    const int units = whole + odd + lone + (r.D - r.rot - lone) / 8, heads = r.heads[0] + r.heads[1];
-    const int per_token = units * heads;
-    for (int i = threadIdx.x; i < count * per_token; i += kThreads) {
-        const int tok = i / per_token, in_tok = i - tok * per_token;
-        const int hh = in_tok / units;
-        int u = in_tok - hh * units;
-        const int64_t bn = first + tok;
+    const int heads = r.heads[0] + r.heads[1];
+    // all heads' pairs, then all heads' copied columns: the lanes of a wave do the same
+    struct Place {
+        const char* in;
+        char* out;
+        int tok, u;
+        bool valid;
+    };
+    auto place = [&](int i, int units) __attribute__((always_inline)) {
+        Place p;
+        const int at = i / units;
+        p.u = i - at * units;
+        p.tok = at / heads;
+        const int hh = at - p.tok * heads, which = hh >= r.heads[0], h = which ? hh - r.heads[0] : hh;
+        const int64_t bn = first + p.tok;
         const int b = (int)(bn / r.N), n = (int)(bn - (int64_t)b * r.N);
-        const int which = hh >= r.heads[0];
-        const int h = which ? hh - r.heads[0] : hh;
-        const char* in = row_of(r.in[which], b, n, h);
-        char* out = row_of(r.out[which], b, n, h);
-        const bool valid = n < user_len(r.lengths, b, r.N);
-        const float2* cs = turn + tok * pairs;
-        if (u < whole) {
+        p.in = row_of(r.in[which], b, n, h);
+        p.out = row_of(r.out[which], b, n, h);
+        p.valid = n < user_len(r.lengths, b, r.N);
+        return p;
+    };
+    const int turned = whole + odd, copied = lone + (r.D - r.rot - lone) / 8;
+    for (int i = threadIdx.x; i < count * heads * turned; i += kThreads) {
+        const Place at = place(i, turned);
+        const float2* cs = turn + at.tok * pairs;
+        const bool valid = at.valid;
+        if (at.u < whole) {
+            const int c = 8 * at.u;
             float x[8], y[8];
             if constexpr (INTERLEAVED) {
-                load8<BF16, true>(in + 8 * u * ES, x);
+                load8<BF16, true>(at.in + c * ES, x);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    const float2 t = cs[4 * u + j];
+                    const float2 t = cs[c / 2 + j];
                     y[2 * j] = valid ? x[2 * j] * t.x - x[2 * j + 1] * t.y : 0.f;
                     y[2 * j + 1] = valid ? x[2 * j + 1] * t.x + x[2 * j] * t.y : 0.f;
                 }
-                store8<BF16, true>(out + 8 * u * ES, y);
+                store8<BF16, true>(at.out + c * ES, y);
             } else {
-                load8<BF16, true>(in + 8 * u * ES, x);
-                load8<BF16, EVEN>(in + (pairs + 8 * u) * ES, y);
+                load8<BF16, true>(at.in + c * ES, x);
+                load8<BF16, EVEN>(at.in + (pairs + c) * ES, y);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    const float2 t = cs[8 * u + j];
+                    const float2 t = cs[c + j];
                     const float a = x[j], d = y[j];
                     x[j] = valid ? a * t.x - d * t.y : 0.f;
                     y[j] = valid ? d * t.x + a * t.y : 0.f;
                 }
-                store8<BF16, true>(out + 8 * u * ES, x);
-                store8<BF16, EVEN>(out + (pairs + 8 * u) * ES, y);
+                store8<BF16, true>(at.out + c * ES, x);
+                store8<BF16, EVEN>(at.out + (pairs + c) * ES, y);
             }
-        } else if (u -= whole; u < odd) {
-            const int p = (INTERLEAVED ? 4 : 8) * whole + u;
+        } else {
+            const int p = (INTERLEAVED ? 4 : 8) * whole + at.u - whole;
             const int ca = INTERLEAVED ? 2 * p : p, cb = INTERLEAVED ? 2 * p + 1 : p + pairs;
             float a = 0.f, d = 0.f;
             if (valid) {
-                a = (float)reinterpret_cast<const E*>(in)[ca];
-                d = (float)reinterpret_cast<const E*>(in)[cb];
+                a = (float)reinterpret_cast<const E*>(at.in)[ca];
+                d = (float)reinterpret_cast<const E*>(at.in)[cb];
                 const float x = a * cs[p].x - d * cs[p].y;
                 d = d * cs[p].x + a * cs[p].y;
                 a = x;
             }
-            reinterpret_cast<E*>(out)[ca] = (E)a;
-            reinterpret_cast<E*>(out)[cb] = (E)d;
-        } else if (valid && !copy) {
-            continue;
-        } else if (u -= odd; u < lone) {
-            reinterpret_cast<E*>(out)[r.rot + u] = valid ? reinterpret_cast<const E*>(in)[r.rot + u] : (E)0.f;
+            reinterpret_cast<E*>(at.out)[ca] = (E)a;
+            reinterpret_cast<E*>(at.out)[cb] = (E)d;
+        }
+    }
+    if (!copy && !r.lengths) return;
+    for (int i = threadIdx.x; i < count * heads * copied; i += kThreads) {
+        const Place at = place(i, copied);
+        if (at.valid && !copy) continue;
+        if (at.u < lone) {
+            const int c = r.rot + at.u;
+            reinterpret_cast<E*>(at.out)[c] = at.valid ? reinterpret_cast<const E*>(at.in)[c] : (E)0.f;
         } else {
-            const int c = r.rot + lone + (u - lone) * 8;
+            const int c = r.rot + lone + (at.u - lone) * 8;
 #pragma unroll
             for (int j = 0; j < ES / 2; ++j) {
                 const v4u zero = {0u, 0u, 0u, 0u};
-                reinterpret_cast<v4u*>(out + c * ES)[j] = valid ? reinterpret_cast<const v4u*>(in + c * ES)[j] : zero;
+                reinterpret_cast<v4u*>(at.out + c * ES)[j] = at.valid ? reinterpret_cast<const v4u*>(at.in + c * ES)[j] : zero;
             }
         }
     }
