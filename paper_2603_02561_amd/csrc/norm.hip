@@ -25,38 +25,42 @@ struct Elem<true> {
     using type = __bf16;
 };
 
-// Columns of vector v, element e of thread t in a team of T: eight in a row where rows start on a vector (VEC), else
-// neighbouring threads take neighbouring columns.
-template <int T, bool VEC>
+// Column of vector v, element e of thread t in a team of T.
+template <int T>
 __device__ __forceinline__ int column(int t, int v, int e) {
-    return VEC ? (v * T + t) * 8 + e : (v * 8 + e) * T + t;
+    return (v * T + t) * 8 + e;
 }
 
-// A team's part of one row as it comes from memory; what lies past d is zero.
+// A team's part of one row as it comes from memory; what lies past d is zero.  VEC: rows start on a vector and end with one.
+// Otherwise the vectors lie wherever the row does (the memory takes that in one access too) and the last one is taken apart.
 template <int T, int NV, bool VEC, bool BF16>
 struct Row {
     static constexpr int VS = BF16 ? 1 : 2;     // 16-byte loads of eight elements
-    v4u raw[VEC ? NV : 1][VS];
-    float one[VEC ? 1 : NV][8];
+    v4u raw[NV][VS];
 
     __device__ __forceinline__ void load(const void* base, size_t at, int d, int t) {
         using E = typename Elem<BF16>::type;
         const E* p = reinterpret_cast<const E*>(base) + at;
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
-            if constexpr (VEC) {
-                const int c = column<T, VEC>(t, v, 0);
+            const int c = column<T>(t, v, 0);
 #pragma unroll
-                for (int j = 0; j < VS; ++j) {
-                    raw[v][j] = v4u{0u, 0u, 0u, 0u};
-                    if (c < d) raw[v][j] = reinterpret_cast<const v4u*>(p + c)[j];
-                }
+            for (int j = 0; j < VS; ++j) raw[v][j] = v4u{0u, 0u, 0u, 0u};
+            if constexpr (VEC) {
+                if (c < d)
+#pragma unroll
+                    for (int j = 0; j < VS; ++j) raw[v][j] = reinterpret_cast<const v4u*>(p + c)[j];
+            } else if (c + 8 <= d) {
+                __builtin_memcpy(raw[v], __builtin_assume_aligned(p + c, sizeof(E)), sizeof(raw[v]));
             } else {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const int c = column<T, VEC>(t, v, e);
-                    one[v][e] = c < d ? (float)p[c] : 0.f;
-                }
+                for (int e = 0; e < 7; ++e)
+                    if (c + e < d) {
+                        if constexpr (BF16)
+                            raw[v][0][e / 2] |= (uint32_t)reinterpret_cast<const uint16_t*>(p)[c + e] << (16 * (e & 1));
+                        else
+                            raw[v][e / 4][e % 4] = __float_as_uint((float)p[c + e]);
+                    }
             }
         }
     }
@@ -65,8 +69,7 @@ struct Row {
         for (int v = 0; v < NV; ++v)
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                if constexpr (!VEC) x[v][e] = one[v][e];
-                else if constexpr (BF16) x[v][e] = e & 1 ? bf16_hi(raw[v][0][e / 2]) : bf16_lo(raw[v][0][e / 2]);
+                if constexpr (BF16) x[v][e] = e & 1 ? bf16_hi(raw[v][0][e / 2]) : bf16_lo(raw[v][0][e / 2]);
                 else x[v][e] = __uint_as_float(raw[v][e / 4][e % 4]);
             }
     }
@@ -78,28 +81,18 @@ __device__ __forceinline__ void store_row(void* base, size_t at, int d, int t, c
     E* p = reinterpret_cast<E*>(base) + at;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
+        const int c = column<T>(t, v, 0);
+        E u[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) u[e] = (E)x[v][e];
         if constexpr (VEC) {
-            const int c = column<T, VEC>(t, v, 0);
-            if (c < d) {
-                if constexpr (BF16) {
-                    v8bf u;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) u[e] = (__bf16)x[v][e];
-                    *reinterpret_cast<v8bf*>(p + c) = u;
-                } else {
-#pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-                        v4f u = {x[v][4 * j], x[v][4 * j + 1], x[v][4 * j + 2], x[v][4 * j + 3]};
-                        reinterpret_cast<v4f*>(p + c)[j] = u;
-                    }
-                }
-            }
+            if (c < d) __builtin_memcpy(__builtin_assume_aligned(p + c, 16), u, sizeof(u));
+        } else if (c + 8 <= d) {
+            __builtin_memcpy(__builtin_assume_aligned(p + c, sizeof(E)), u, sizeof(u));
         } else {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int c = column<T, VEC>(t, v, e);
-                if (c < d) p[c] = (E)x[v][e];
-            }
+            for (int e = 0; e < 7; ++e)
+                if (c + e < d) p[c + e] = u[e];
         }
     }
 }
@@ -144,7 +137,7 @@ __global__ __launch_bounds__(block_for(T)) void layer_norm_kernel(const void* in
     for (int v = 0; v < NV; ++v)
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const int c = column<T, VEC>(t, v, e);
+            const int c = column<T>(t, v, e);
             w[v][e] = weight && c < d ? weight[(size_t)group * d + c] : 1.f;
             b[v][e] = bias && c < d ? bias[(size_t)group * d + c] : 0.f;
         }
@@ -167,7 +160,7 @@ __global__ __launch_bounds__(block_for(T)) void layer_norm_kernel(const void* in
         for (int v = 0; v < NV; ++v)
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                x[v][e] = column<T, VEC>(t, v, e) < d ? x[v][e] - mu : 0.f;
+                x[v][e] = column<T>(t, v, e) < d ? x[v][e] - mu : 0.f;
                 s[0] = fmaf(x[v][e], x[v][e], s[0]);
             }
         team_sum<T, 1>(s, part, turn);
@@ -201,7 +194,7 @@ __global__ __launch_bounds__(block_for(T)) void layer_norm_backward_kernel(
     for (int v = 0; v < NV; ++v)
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const int c = column<T, VEC>(t, v, e);
+            const int c = column<T>(t, v, e);
             w[v][e] = weight && c < d ? weight[(size_t)group * d + c] : 1.f;
             dw[v][e] = db[v][e] = 0.f;
         }
@@ -231,7 +224,7 @@ __global__ __launch_bounds__(block_for(T)) void layer_norm_backward_kernel(
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 // past d dy is zero, and a zero takes the place of what x would give there
-                x[v][e] = column<T, VEC>(t, v, e) < d ? (x[v][e] - mu) * rs : 0.f;
+                x[v][e] = column<T>(t, v, e) < d ? (x[v][e] - mu) * rs : 0.f;
                 const float a = dy[v][e] * w[v][e];
                 s[0] += a;
                 s[1] = fmaf(a, x[v][e], s[1]);
@@ -258,7 +251,7 @@ __global__ __launch_bounds__(block_for(T)) void layer_norm_backward_kernel(
 #pragma unroll
             for (int v = 0; v < NV; ++v)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) sums[team][column<T, VEC>(t, v, e)] = mine[v][e];
+                for (int e = 0; e < 8; ++e) sums[team][column<T>(t, v, e)] = mine[v][e];
             __syncthreads();
             for (int c = threadIdx.x; c < d; c += block_for(T)) {
                 float s = 0.f;
@@ -314,10 +307,11 @@ int teams_for(int rows, int groups, int d) {
 }
 
 // Workgroups of the gradient for each group: their sums for dw and db are written once each, so there are no more than keep
-// the GPU busy (1024 together), and none whose teams would have less than four rows.
+// the GPU busy (512 together: 32768 rows of 4096 take 156 us, with 1024 185, as three of them fit a compute unit), and none whose
+// teams would have less than four rows.
 int blocks_for(int rows, int groups, int d) {
     const int per_block = block_for(team_for(d).threads) / team_for(d).threads;
-    const int want = ceil_div(1024, groups), most = ceil_div(rows, 4 * per_block);
+    const int want = ceil_div(512, groups), most = ceil_div(rows, 4 * per_block);
     return want < most ? want : most;
 }
 
