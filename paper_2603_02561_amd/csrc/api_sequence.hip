@@ -66,7 +66,7 @@ solar_status check_decay(int B, int N, int H, int Hkv, int D, float scale, solar
 
 struct DecayCarve {
     DecayParts cut;
-    float *parts, *part_moments;    // [B,H,parts,D,D], none for one part
+    float *parts, *part_moments;    // [B,H,parts * pieces,D,D], none for one part
     float *dk, *dv;                 // [B,N,H,D] of every head, where heads share K and V
     double* moments;                // [B,H,parts,slices]
     size_t total;
@@ -82,7 +82,7 @@ DecayCarve carve_decay(void* ws, int B, int N, int H, int Hkv, int D, bool backw
     };
     if (!backward && N <= kDecayRows) return c;
     c.cut = decay_parts(B, N, H, D, backward ? 2 : 1);
-    const size_t states = c.cut.parts > 1 ? (size_t)B * H * c.cut.parts * D * D : 0;
+    const size_t states = c.cut.parts > 1 ? (size_t)B * H * c.cut.parts * c.cut.pieces * D * D : 0;
     c.parts = part(states);
     if (backward) {
         const size_t shared = H != Hkv ? (size_t)B * N * H * D : 0;
@@ -198,6 +198,7 @@ solar_status solar_decay_attention(const void* Q, const void* K, const void* V, 
     w.bf16 = t == SOLAR_BF16;
     w.nparts = c.cut.parts;
     w.part_rows = c.cut.rows;
+    w.pieces = c.cut.pieces;
     w.parts = c.parts;
     const hipError_t e = N <= kDecayRows ? launch_decay_rows(w, (hipStream_t)stream)
                                          : launch_decay_chunks({{w}, 1}, (hipStream_t)stream);
@@ -237,6 +238,7 @@ solar_status solar_decay_attention_backward(const void* Q, const void* K, const 
     w.bf16 = t == SOLAR_BF16;
     w.nparts = c.cut.parts;
     w.part_rows = c.cut.rows;
+    w.pieces = c.cut.pieces;
     w.parts = c.parts;
     w.part_moments = c.part_moments;
     // dq_t = scale S_t do_t: the same walk with do for q, v for k and k for v, its state transposed

@@ -247,17 +247,19 @@ decay_chunk_kernel(Walks ws) {
     // they find each other's rows in its L2.
     const int turn = blockIdx.x >> 3, slice = turn % NS, k0 = turn / NS / ws.count;
     const Walk& w = ws.walk[turn / NS % ws.count];
-    const int share = ws.walk[0].k.share, nparts = MODE == kLast ? 1 : STATES ? w.nparts - 1 : w.nparts;
+    // the states in front of the last part are formed in shorter pieces, w.pieces of them to a part
+    const int pieces = STATES ? w.pieces : 1, part_rows = STATES ? w.part_rows / w.pieces : w.part_rows;
+    const int share = ws.walk[0].k.share, nparts = MODE == kLast ? 1 : STATES ? (w.nparts - 1) * pieces : w.nparts;
     const int64_t unit = (int64_t)(k0 / share * 8 + (blockIdx.x & 7)) * share + k0 % share;
     if (unit >= (int64_t)w.B * w.H * nparts) return;
     const int h = (int)(unit % w.H), b = (int)(unit / w.H / nparts);
     // in the order of the walk; the last part's state is nobody's start
-    const int order = MODE == kLast ? w.nparts - 1 : (int)(unit / w.H % nparts), part = w.reverse ? w.nparts - 1 - order : order;
+    const int order = MODE == kLast ? w.nparts - 1 : (int)(unit / w.H % nparts), part = w.reverse ? w.nparts * pieces - 1 - order : order;
 
     const int tid = threadIdx.x, wave = tid >> 6;
     const int len = user_len(w.lengths, b, w.N);
-    const int row0 = part * w.part_rows;
-    const int rows = w.N - row0 < w.part_rows ? w.N - row0 : w.part_rows;
+    const int row0 = part * part_rows;
+    const int rows = w.N - row0 < part_rows ? w.N - row0 : part_rows;   // below 0 for a piece past the end
     const int count = len - row0 < 0 ? 0 : (len - row0 < rows ? len - row0 : rows);
     const int pre = w.reverse ? 0 : 1;
     const float lg = w.log_decay[h];
@@ -284,7 +286,7 @@ decay_chunk_kernel(Walks ws) {
     auto column = [](int c16, int nb) { return NB == 2 ? 8 * (c16 >> 2) + 4 * nb + (c16 & 3) : 16 * nb + c16; };
     v4f S[NJ][NB][2], T[MJ][MB][2];
     const size_t state_at = ((size_t)b * w.H + h) * D * D;
-    const size_t part_at = (((size_t)b * w.H + h) * w.nparts + order) * D * D;
+    const size_t part_at = (((size_t)b * w.H + h) * w.nparts * w.pieces + (STATES ? order : order * w.pieces)) * D * D;
     // f(the place of an entry in a state, the same in a transposed one, j, nb, a, i)
     auto entries = [&](auto f) __attribute__((always_inline)) {
         const int c16 = tid & 15, g4 = tid >> 4 & 3;
@@ -701,8 +703,8 @@ decay_chunk_kernel(Walks ws) {
     }
 }
 
-// parts[o] holds the state behind part o of the walk from a zero state (nothing yet for the last part); it becomes the state that
-// part o starts from.
+// parts[o] holds the state behind piece o of the walk from a zero state, for the pieces of all parts but the last; the first piece
+// of every part, the last part's too, becomes the state that the part starts from.
 template <bool MOMENT>
 __global__ __launch_bounds__(kJoinThreads) void join_parts_kernel(Walk w) {
     const int DD = w.D * w.D;
@@ -713,24 +715,25 @@ __global__ __launch_bounds__(kJoinThreads) void join_parts_kernel(Walk w) {
     const size_t bh = (size_t)b * w.H + h;
     float s = 0.f, t = 0.f;
     if (w.state_in) s = w.state_in[bh * DD + (w.in_turned ? (e % w.D) * w.D + e / w.D : e)];
-    float* p = w.parts + bh * w.nparts * DD + e;
-    float* pm = MOMENT ? w.part_moments + bh * w.nparts * DD + e : nullptr;
-    for (int o = 0; o + 1 < w.nparts; ++o) {
-        const int part = w.reverse ? w.nparts - 1 - o : o, row0 = part * w.part_rows;
-        const int rows = w.N - row0 < w.part_rows ? w.N - row0 : w.part_rows;
+    const int all = w.nparts * w.pieces, last = all - w.pieces, piece_rows = w.part_rows / w.pieces;
+    float* p = w.parts + bh * all * DD + e;
+    float* pm = MOMENT ? w.part_moments + bh * all * DD + e : nullptr;
+    for (int o = 0; o < last; ++o) {
+        const int part = w.reverse ? all - 1 - o : o, row0 = part * piece_rows;
+        const int rows = w.N - row0 < piece_rows ? w.N - row0 : piece_rows;
         const int count = len - row0 < 0 ? 0 : (len - row0 < rows ? len - row0 : rows);
         const float g = expm1f(lg * (float)count), gc = count ? g : 0.f;      // log g may be -infinity
         if constexpr (MOMENT) {
             const float add = pm[(size_t)o * DD], x = fmaf((float)count, s, t);
-            pm[(size_t)o * DD] = t;
+            if (o % w.pieces == 0) pm[(size_t)o * DD] = t;
             t = fmaf(x, gc, x) + add;
         }
         const float add = p[(size_t)o * DD];
-        p[(size_t)o * DD] = s;
+        if (o % w.pieces == 0) p[(size_t)o * DD] = s;
         s = fmaf(s, gc, s) + add;
     }
-    p[(size_t)(w.nparts - 1) * DD] = s;
-    if constexpr (MOMENT) pm[(size_t)(w.nparts - 1) * DD] = t;
+    p[(size_t)last * DD] = s;
+    if constexpr (MOMENT) pm[(size_t)last * DD] = t;
 }
 
 template <int D, bool BF16, int MODE>
@@ -755,7 +758,8 @@ hipError_t run(const Walks& ws, hipStream_t stream) {
     if (w.nparts > 1) {
         Walks one = ws;
         one.count = 1;
-        e = w.moment ? launch<D, BF16, kMomentState>(one, w.nparts - 1, stream) : launch<D, BF16, kState>(one, w.nparts - 1, stream);
+        e = w.moment ? launch<D, BF16, kMomentState>(one, (w.nparts - 1) * w.pieces, stream)
+                     : launch<D, BF16, kState>(one, (w.nparts - 1) * w.pieces, stream);
         if (e != hipSuccess) return e;
         const dim3 grid((unsigned)((size_t)w.B * w.H * D * D / kJoinThreads));
         if (w.moment) hipLaunchKernelGGL(join_parts_kernel<true>, grid, dim3(kJoinThreads), 0, stream, w);
@@ -783,15 +787,22 @@ int moment_slices(int D) { return D == 256 ? 4 : 1; }
 
 // Parts that a sequence is cut into.  Two workgroups of the kernel fit a compute unit, so 512 fill the GPU; every part but
 // the last reads K and V once more, so there are no more than that takes, and none below 128 rows.  `walks` of them run in one
-// launch.
+// launch.  The states in front of the last part are formed by one walk only; where its parts are few they are cut further, into
+// up to four pieces of at least 256 rows (8 x 4096 rows of 16 heads at D = 128: 84 -> 42 us for 128 parts in four pieces).
 DecayParts decay_parts(int B, int N, int H, int D, int walks) {
-    const int64_t have = (int64_t)B * H * (D == 256 ? 2 : 1) * walks;
+    const int64_t heads = (int64_t)B * H * (D == 256 ? 2 : 1), have = heads * walks;
     int64_t n = (512 + have - 1) / have;
     const int64_t most = N / 128;
     if (n > most) n = most;
-    if (n < 1) n = 1;
-    const int rows = (int)((((int64_t)N + n - 1) / n + 63) / 64 * 64);
-    return {ceil_div(N, rows), rows};
+    if (n < 2) return {1, (N + 63) / 64 * 64, 1};
+    const int64_t rows = (N + n - 1) / n;
+    int64_t pieces = 512 / (heads * (n - 1));
+    if (pieces > 4) pieces = 4;
+    if (pieces > rows / 256) pieces = rows / 256;
+    if (pieces < 1) pieces = 1;
+    const int64_t unit = 64 * pieces;
+    const int part_rows = (int)((rows + unit - 1) / unit * unit);
+    return {ceil_div(N, part_rows), part_rows, (int)pieces};
 }
 
 }  // namespace solar

@@ -36,9 +36,9 @@ struct Walk {
     float o_scale, kv_scale;
     bool reverse, in_turned;        // in_turned: state_in is read transposed
     bool bf16, o_float;             // o_float: o is float whatever the inputs are
-    // the sequence is cut into nparts parts of part_rows rows (a multiple of 64); parts and part_moments are
-    // [B,H,nparts,D,D] work arrays, not used where nparts is 1
-    int nparts, part_rows;
+    // the sequence is cut into nparts parts of part_rows rows, and each part into `pieces` pieces of a multiple of 64; parts and
+    // part_moments are [B,H,nparts * pieces,D,D] work arrays, not used where nparts is 1
+    int nparts, part_rows, pieces;
     float *parts, *part_moments;
     bool parts_turned;              // parts hold the states of this walk transposed
     // moment: also the derivative of o by log g, summed against `grad`, and that of the last state against `grad_state` (or null;
@@ -71,7 +71,7 @@ hipError_t launch_share_sum(const float* in, int B, int N, int H, int Hkv, int D
 
 // decay_chunk.hip
 struct DecayParts {
-    int parts, rows;
+    int parts, rows, pieces;
 };
 DecayParts decay_parts(int B, int N, int H, int D, int walks);
 int moment_slices(int D);

@@ -429,3 +429,31 @@ def test_gradients_after_a_nan_leave_later_rows(lib, dtype, D):
         assert not torch.isfinite(got[i][0, 100]).all()
     keep = torch.arange(200) != 100
     assert torch.equal(got[0].cpu()[0, keep], want[0].cpu()[0, keep]) and torch.isnan(got[0][0, 100]).any()
+
+
+@pytest.mark.parametrize("reverse_states", [False, True])
+def test_many_heads_as_the_same_users_alone(lib, reverse_states):
+    """With 64 heads a long sequence is cut into few parts whose states are formed in pieces; one user alone is cut into many
+    parts.  Either result is off by at most (N + 2 D + 16) u < 1.4e-4 of the sums of absolute values; standard normal terms of either
+    sign leave sums of more than a hundredth of those, and roundings of either sign no more than a hundredth of the bound: 2e-4 of
+    the 2-norm is far above both together, and far below what a piece too many or too few would do."""
+    N = 2100
+    p = Problem(4, N, 16, 8, 64, "f32", lengths=[N, 1700, 0, 600], state=True, seed=17, backward=True).garbage()
+    if not reverse_states:
+        p.dstate = torch.zeros_like(p.dstate)
+    all_o, all_s = forward(lib, p)
+    all_g = backward(lib, p)
+    dlog = torch.zeros(16, device="cuda", dtype=torch.float64)
+    near = lambda a, b: (a.double() - b.double()).norm() <= 2e-4 * b.double().norm()  # noqa: E731
+    for i in range(4):
+        one = Problem(1, N, 16, 8, 64, "f32", backward=True)
+        for name in ("q", "k", "v", "do", "state", "dstate", "lengths"):
+            setattr(one, name, getattr(p, name)[i:i + 1].clone())
+        one.log_decay, one.scale = p.log_decay, p.scale
+        o, s = forward(lib, one)
+        assert near(all_o[i], o[0]) and near(all_s[i], s[0]), i
+        g = backward(lib, one)
+        for a, b in zip(all_g[:4], g[:4]):
+            assert near(a[i], b[0]), i
+        dlog += g[4].double()
+    assert near(all_g[4], dlog)
