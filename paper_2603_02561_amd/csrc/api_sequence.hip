@@ -145,6 +145,12 @@ solar_status solar_rotary(const void* Q, const void* K, const int32_t* lengths, 
     if (K && (!take(K, strides ? strides + 1 : nullptr, B, N, Hkv, D, es, 1, false, &r.in[1]) ||
               !take(Kout, strides ? strides + 3 : nullptr, B, N, Hkv, D, es, 1, true, &r.out[1])))
         return SOLAR_ERR_INVALID_ARG;
+    // in place only with the same places, and not one over the other
+    for (int i = 0; i < (K ? 2 : 1); ++i)
+        if (r.in[i].data == r.out[i].data && (r.in[i].s.batch != r.out[i].s.batch || r.in[i].s.row != r.out[i].s.row ||
+                                              r.in[i].s.head != r.out[i].s.head))
+            return SOLAR_ERR_INVALID_ARG;
+    if (K && (Qout == K || Kout == Q || Qout == Kout)) return SOLAR_ERR_INVALID_ARG;
     if ((int64_t)B * N > kMaxBlocks || (int64_t)H + (K ? Hkv : 0) > 65536) return SOLAR_ERR_UNSUPPORTED;
     r.heads[0] = H;
     r.heads[1] = K ? Hkv : 0;
@@ -172,6 +178,7 @@ solar_status solar_decay_attention(const void* Q, const void* K, const void* V, 
     if (v != SOLAR_OK) return v;
     if (!log_decay || !K || !V || (!O && !state_out) || (O && !Q)) return SOLAR_ERR_INVALID_ARG;
     if (misaligned(state_in, 16) || misaligned(state_out, 16)) return SOLAR_ERR_INVALID_ARG;
+    if (O && (O == Q || O == K || O == V)) return SOLAR_ERR_INVALID_ARG;     // other workgroups still read what O's rows replace
     const size_t es = t == SOLAR_BF16 ? 2 : 4;
     const int share = H / Hkv;
     Walk w = {};
@@ -215,6 +222,11 @@ solar_status solar_decay_attention_backward(const void* Q, const void* K, const 
     if (v != SOLAR_OK) return v;
     if (!log_decay) return SOLAR_ERR_INVALID_ARG;
     if (misaligned(state_in, 16) || misaligned(dstate_out, 16) || misaligned(dstate_in, 16)) return SOLAR_ERR_INVALID_ARG;
+    for (const void* out : {dQ, dK, dV})
+        for (const void* in : {Q, K, V, dO})
+            if (out == in) return SOLAR_ERR_INVALID_ARG;
+    if (dQ == dK || dQ == dV || dK == dV || (dstate_in && (dstate_in == dstate_out || dstate_in == state_in)))
+        return SOLAR_ERR_INVALID_ARG;
     const size_t es = t == SOLAR_BF16 ? 2 : 4;
     const int share = H / Hkv;
     auto at = [&](int i) { return strides ? strides + i : nullptr; };
@@ -302,6 +314,7 @@ solar_status solar_layer_norm(const void* In, const float* weight, const float* 
     if (!In || !Out || misaligned(In, 16) || misaligned(Out, 16) || !known(t_in) || !known(t_out) || !(eps >= 0.f) ||
         !std::isfinite(eps))
         return SOLAR_ERR_INVALID_ARG;
+    if (Out == In && t_in != t_out) return SOLAR_ERR_INVALID_ARG;
     return launch_layer_norm(In, weight, bias, rows, groups, d, eps, t_in == SOLAR_BF16, t_out == SOLAR_BF16, Out, mean,
                              rstd, (hipStream_t)stream) == hipSuccess ? SOLAR_OK : SOLAR_ERR_HIP;
 }
@@ -320,6 +333,7 @@ solar_status solar_layer_norm_backward(const void* In, const float* weight, cons
     if (!In || !mean || !rstd || !dOut || !dIn || misaligned(In, 16) || misaligned(dOut, 16) || misaligned(dIn, 16) ||
         !known(t_in) || !known(t_out))
         return SOLAR_ERR_INVALID_ARG;
+    if (dIn == dOut && t_in != t_out) return SOLAR_ERR_INVALID_ARG;
     if (dweight || dbias) {
         const size_t need = solar_layer_norm_workspace_bytes(rows, groups, d);
         if (!workspace || workspace_bytes < need || misaligned(workspace, 256)) return SOLAR_ERR_WORKSPACE;

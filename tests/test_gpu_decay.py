@@ -457,3 +457,23 @@ def test_many_heads_as_the_same_users_alone(lib, reverse_states):
             assert near(a[i], b[0]), i
         dlog += g[4].double()
     assert near(all_g[4], dlog)
+
+
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_gradients_and_nans_in_the_inputs(lib, dtype, D):
+    """Which rows of which gradient a NaN in row 100 of an input may reach; the others are equal bit for bit."""
+    p = Problem(1, 200, 1, 1, D, dtype, seed=7, backward=True)
+    want = [x.cpu() for x in backward(lib, p)[:3]]
+    row = torch.arange(200)
+    # untouched rows of dQ, dK, dV
+    rules = {"q": (row >= 0, row > 100, row > 100), "k": (row < 100, row >= 0, row != 100), "v": (row < 100, row != 100, row >= 0)}
+    for name, kept in rules.items():
+        x = getattr(p, name)
+        before = x[0, 100, 0, 5].clone()
+        x[0, 100, 0, 5] = float("nan")
+        got = [y.cpu() for y in backward(lib, p)[:3]]
+        x[0, 100, 0, 5] = before
+        for i in range(3):
+            assert torch.equal(got[i][0, kept[i]], want[i][0, kept[i]]), (name, i)
+            assert kept[i].all() or not torch.isfinite(got[i][0, 100]).all(), (name, i)

@@ -119,34 +119,37 @@ def test_refusals(lib):
     """Every entry point's argument errors, on the host: nothing is launched, and no pointer is followed."""
     L = lib._lib
     p, bad = 0x1000, 0x1004
+    p2, p3, p4, p5, p6, p7 = (0x1000 * i for i in range(2, 8))
     OK, INVALID, UNSUPPORTED, WORKSPACE = 0, 1, 2, 3
 
     def strides(*v):
         return (ctypes.c_int64 * len(v))(*v)
 
     def rotary(**k):
-        a = dict(Q=p, K=p, lengths=None, positions=None, freq=p, B=2, N=3, H=4, Hkv=2, D=64, rot=64, layout=0, inverse=0,
-                 amplitude=1.0, t=0, strides=None, Qout=p, Kout=p, stream=None)
+        a = dict(Q=p, K=p2, lengths=None, positions=None, freq=p, B=2, N=3, H=4, Hkv=2, D=64, rot=64, layout=0, inverse=0,
+                 amplitude=1.0, t=0, strides=None, Qout=p, Kout=p2, stream=None)
         a.update(k)
         return L.solar_rotary(*a.values())
 
     for k in ({"Q": None}, {"Qout": None}, {"freq": None}, {"freq": bad}, {"B": 0}, {"N": 0}, {"H": 0}, {"Hkv": 0}, {"D": 0}, {"rot": 0}, {"rot": 7},
               {"rot": 66}, {"layout": 2}, {"t": 5}, {"amplitude": float("nan")}, {"Kout": None}, {"K": None}, {"Q": bad},
               {"Kout": bad}, {"strides": strides(*([0, 0, 0] * 4))}, {"strides": strides(768, 256, 66, *([768, 256, 64] * 3))},
-              {"strides": strides(768, 256, -64, *([768, 256, 64] * 3))}):
+              {"strides": strides(768, 256, -64, *([768, 256, 64] * 3))},
+              # in place with other strides, one over the other
+              {"strides": strides(1536, 512, 128, 384, 128, 64, 768, 256, 64, 384, 128, 64)}, {"Kout": p}, {"Qout": p2}):
         assert rotary(**k) == INVALID, k
     for k in ({"D": 68}, {"D": 520, "rot": 64}, {"B": 1 << 13, "N": 1 << 13}):
         assert rotary(**k) == UNSUPPORTED, k
 
     def decay(**k):
-        a = dict(Q=p, K=p, V=p, log_decay=p, lengths=None, state_in=None, B=2, N=3, H=4, Hkv=2, D=64, scale=1.0, t=1,
-                 strides=None, O=p, state_out=None, workspace=0x1000, bytes=1 << 40, stream=None)
+        a = dict(Q=p, K=p2, V=p3, log_decay=p, lengths=None, state_in=None, B=2, N=3, H=4, Hkv=2, D=64, scale=1.0, t=1,
+                 strides=None, O=p4, state_out=None, workspace=0x1000, bytes=1 << 40, stream=None)
         a.update(k)
         return L.solar_decay_attention(*a.values())
 
     for k in ({"Q": None}, {"K": None}, {"V": None}, {"log_decay": None}, {"O": None}, {"B": 0}, {"N": -1}, {"H": 0},
               {"Hkv": 3}, {"Hkv": 0}, {"D": 0}, {"scale": float("inf")}, {"t": 2}, {"Q": bad}, {"K": bad}, {"O": bad},
-              {"state_in": bad}, {"state_out": bad}, {"strides": strides(768, 256, 64, *([384, 128, 64] * 2), 768, 64, 64)},
+              {"state_in": bad}, {"state_out": bad}, {"O": p}, {"O": p2}, {"O": p3}, {"strides": strides(768, 256, 64, *([384, 128, 64] * 2), 768, 64, 64)},
               {"strides": strides(768, 256, 64, 384, 128, 63, 384, 128, 64, 768, 256, 64)}):
         assert decay(**k) == INVALID, k
     for k in ({"D": 32}, {"D": 96}, {"D": 512}, {"B": 1 << 20, "H": 64}):
@@ -154,38 +157,39 @@ def test_refusals(lib):
     assert lib.solar_decay_workspace_bytes(2, 3, 4, 2, 96, 1, False) == 0
 
     def decay_bw(**k):
-        a = dict(Q=p, K=p, V=p, dO=p, log_decay=p, lengths=None, state_in=None, dstate_out=None, B=2, N=3, H=4, Hkv=2, D=64,
-                 scale=1.0, t=1, strides=None, dQ=p, dK=p, dV=p, dstate_in=None, dlog_decay=None, workspace=0x1000,
+        a = dict(Q=p, K=p2, V=p3, dO=p4, log_decay=p, lengths=None, state_in=None, dstate_out=None, B=2, N=3, H=4, Hkv=2, D=64,
+                 scale=1.0, t=1, strides=None, dQ=p5, dK=p6, dV=p7, dstate_in=None, dlog_decay=None, workspace=0x1000,
                  bytes=1 << 40, stream=None)
         a.update(k)
         return L.solar_decay_attention_backward(*a.values())
 
     for k in ({"Q": None}, {"dO": None}, {"dQ": None}, {"dK": None}, {"dV": None}, {"log_decay": None}, {"Hkv": 3},
-              {"dstate_out": bad}, {"dstate_in": bad}, {"dV": bad}, {"t": 9}, {"scale": float("nan")}):
+              {"dstate_out": bad}, {"dstate_in": bad}, {"dV": bad}, {"t": 9}, {"scale": float("nan")}, {"dQ": p4}, {"dK": p2}, {"dV": p6}, {"dstate_in": p, "dstate_out": p},
+              {"dstate_in": p, "state_in": p}):
         assert decay_bw(**k) == INVALID, k
     assert decay_bw(D=72) == UNSUPPORTED
     for k in ({"workspace": None}, {"workspace": 0x1010}, {"bytes": 16}):
         assert decay_bw(**k) == WORKSPACE, k
 
     def norm(**k):
-        a = dict(In=p, weight=None, bias=None, rows=3, groups=2, d=64, eps=1e-5, t_in=0, t_out=1, Out=p, mean=None, rstd=None,
+        a = dict(In=p, weight=None, bias=None, rows=3, groups=2, d=64, eps=1e-5, t_in=0, t_out=1, Out=p2, mean=None, rstd=None,
                  stream=None)
         a.update(k)
         return L.solar_layer_norm(*a.values())
 
     for k in ({"In": None}, {"Out": None}, {"In": bad}, {"Out": bad}, {"rows": 0}, {"groups": 0}, {"d": 0}, {"eps": -1.0},
-              {"eps": float("nan")}, {"t_in": 2}, {"t_out": -1}):
+              {"eps": float("nan")}, {"t_in": 2}, {"t_out": -1}, {"Out": p}):
         assert norm(**k) == INVALID, k
     for k in ({"d": 16385}, {"groups": 1 << 20, "d": 512}, {"rows": 1 << 30, "groups": 2}):
         assert norm(**k) == UNSUPPORTED, k
 
     def norm_bw(**k):
-        a = dict(In=p, weight=None, mean=p, rstd=p, dOut=p, rows=3, groups=2, d=64, t_in=0, t_out=1, dIn=p, dweight=p,
+        a = dict(In=p, weight=None, mean=p, rstd=p, dOut=p2, rows=3, groups=2, d=64, t_in=0, t_out=1, dIn=p3, dweight=p,
                  dbias=None, workspace=0x1000, bytes=1 << 40, stream=None)
         a.update(k)
         return L.solar_layer_norm_backward(*a.values())
 
-    for k in ({"In": None}, {"mean": None}, {"rstd": None}, {"dOut": None}, {"dIn": None}, {"dIn": bad}, {"t_in": 3}):
+    for k in ({"In": None}, {"mean": None}, {"rstd": None}, {"dOut": None}, {"dIn": None}, {"dIn": bad}, {"t_in": 3}, {"dIn": p2}):
         assert norm_bw(**k) == INVALID, k
     for k in ({"workspace": None}, {"workspace": 0x1010}, {"bytes": 8}):
         assert norm_bw(**k) == WORKSPACE, k
