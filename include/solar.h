@@ -306,7 +306,8 @@ solar_status solar_svd_factorize_rsvd(const void* X, const int32_t* lengths, int
  * a decay (the ordered form of solar_linear_attention, with a state that a server keeps between rows), layer norm of its
  * heads; each with its gradient.  What differs from the conventions above: Q, K, V and their like are tensors of heads
  * [B,N,heads,D], may lie in memory with strides, and outputs that take their place in the next operator have the inputs'
- * type t (bf16 rounded to nearest even).  H is a multiple of Hkv; head h reads head h / (H / Hkv) of K and V.
+ * type t (bf16 rounded to nearest even).  H is a multiple of Hkv; head h reads head h / (H / Hkv) of K and V.  There is no
+ * `info`: an entry of `lengths` outside [0, N] is taken as the nearer of the two.
  *
  * Elements between neighbouring users, rows and heads of a tensor of heads; its D columns are contiguous.  [B,N,heads,D]
  * in order, [B,heads,N,D], and slices of a packed projection are all described so.  A stride is not negative and a

@@ -477,3 +477,12 @@ def test_gradients_and_nans_in_the_inputs(lib, dtype, D):
         for i in range(3):
             assert torch.equal(got[i][0, kept[i]], want[i][0, kept[i]]), (name, i)
             assert kept[i].all() or not torch.isfinite(got[i][0, 100]).all(), (name, i)
+
+
+@pytest.mark.parametrize("N", [3, 100, 1500])
+def test_lengths_out_of_range_are_the_nearer_end(lib, N):
+    p = Problem(3, N, 2, 2, 64, "bf16", lengths=[-7, N + 1000, 2], state=True, seed=2)
+    o, s = forward(lib, p)
+    p.lengths = torch.tensor([0, N, 2], dtype=torch.int32)
+    o2, s2 = forward(lib, p)
+    assert torch.equal(o, o2) and torch.equal(s, s2)
