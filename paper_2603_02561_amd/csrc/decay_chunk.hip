@@ -8,9 +8,8 @@
 // read; only P = Q K^T o M goes through LDS, each wave forming a share of it.
 //
 // Precision.  Sums and S are float.  The matrix unit takes bf16, so a float operand is cut into bf16 terms that add up to it:
-// three (24 bits) where the sum stays float - the state - and for float inputs, whose products take the six pairs of terms
-// above 2^-24; two (16 bits) for S and P where the result is rounded to bf16 anyway (2^-8).  g^C S is S + (g^C - 1) S, so that
-// the error of a rounded g^C does not add up over the chunks.
+// three, which hold all 24 bits.  Products of two such operands (float inputs) take the six pairs of terms above 2^-24.  g^C S is
+// S + (g^C - 1) S, so that the error of a rounded g^C does not add up over the chunks.
 //
 // What bounds it: not memory (64 users of 10000 rows at D = 128: 655 MB, 130 us at the rate of a copy; 190 us, of which the kernel
 // without its loads and stores takes 155) but the instructions of a chunk: per wave 204 matrix instructions, 3300 cycles, and 800 of
@@ -38,7 +37,7 @@ struct ChunkCfg {
     static constexpr int NB = D == 128 && !MOMENT ? 2 : 1;
     static constexpr int kThreads = 4 * W / NB;
     static constexpr int NT = BF16 ? 1 : 3;                             // terms of an input
-    static constexpr int TP = BF16 ? 2 : 3;                             // terms of P and S where they meet V and Q
+    static constexpr int TP = 3;                                        // terms of P and S where they meet V and Q
     static constexpr int LP = C + 8;                                    // bf16 per row of P's images
     static constexpr int kQ = NT * C * D, kV = NT * C * W, kP = (TP + (MOMENT ? 3 : 0)) * C * LP;
     static constexpr int kTables = 4 * C + 3 + 16;
