@@ -385,7 +385,8 @@ solar_status solar_decay_attention(const void* Q, const void* K, const void* V, 
  *   strides     in HOST memory [7]: Q, K, V, dO, dQ, dK, dV; NULL: all contiguous
  *   dQ, dK, dV  out, of type t, rows at or past the valid length zero
  *   dstate_in   out [B,H,D,D] float or NULL       dlog_decay  out [H] float or NULL
- * Outputs overlap nothing.  Workspace: solar_decay_workspace_bytes(B, N, H, Hkv, D, t, 1), 256-byte aligned.
+ * Outputs overlap nothing.  Workspace: solar_decay_workspace_bytes(B, N, H, Hkv, D, t, 1), 256-byte aligned.  It may be less
+ * than the operator's own: a buffer for both takes the larger of the two.
  */
 solar_status solar_decay_attention_backward(const void* Q, const void* K, const void* V, const void* dO,
                                             const float* log_decay, const int32_t* lengths, const float* state_in,

@@ -567,9 +567,11 @@ class SequenceMixer:
         self.state = torch.zeros((B, H, D, D), dtype=torch.float32, device=dev)
         self.positions = torch.zeros((B, 1), dtype=torch.int32, device=dev)
         code = SOLAR_BF16 if dtype == torch.bfloat16 else SOLAR_F32
-        nbytes = solar_decay_workspace_bytes(B, N, H, Hkv, D, code, training)
+        # neither direction's need is a bound of the other's: they cut a sequence into parts of their own
+        nbytes = solar_decay_workspace_bytes(B, N, H, Hkv, D, code, False)
         if training:
-            nbytes = max(nbytes, solar_layer_norm_workspace_bytes(B * N, H, D))
+            nbytes = max(nbytes, solar_decay_workspace_bytes(B, N, H, Hkv, D, code, True),
+                         solar_layer_norm_workspace_bytes(B * N, H, D))
             self.dO = empty(B, N, H, D, dtype=dtype)
             self.dQ, self.dK, self.dV = (empty(B, N, h, D, dtype=dtype) for h in (H, Hkv, Hkv))
             self.dweight, self.dbias, self.dlog_decay = empty(H, D), empty(H, D), empty(H)

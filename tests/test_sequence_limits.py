@@ -1,0 +1,57 @@
+"""The sequence operators' workspaces and limits on the host: no GPU is needed, nothing is launched and no pointer is followed."""
+import ctypes
+
+import pytest
+import torch
+
+OK, INVALID, UNSUPPORTED, WORKSPACE = 0, 1, 2, 3
+P = [0x1000 * (i + 1) for i in range(12)]
+
+
+@pytest.fixture(scope="module")
+def lib():
+    from paper_2603_02561_amd import binding
+    return binding
+
+
+def strides(*v):
+    return (ctypes.c_int64 * len(v))(*v)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("training", [False, True])
+def test_the_mixer_has_the_workspace_of_both_directions(lib, training, dtype):
+    code = lib.SOLAR_BF16 if dtype == torch.bfloat16 else lib.SOLAR_F32
+    for D in (64, 128, 256):
+        for B, H, Hkv in ((1, 1, 1), (3, 4, 2), (16, 8, 8), (16, 16, 16), (16, 16, 4), (43, 6, 6), (15, 17, 17), (73, 7, 7), (32, 16, 16), (64, 32, 8)):
+            lg, freq = torch.empty(H, device="meta"), torch.empty(D // 2, dtype=torch.float64, device="meta")
+            w = torch.empty(H, D, device="meta")
+            for N in (1, 4, 5, 127, 255, 256, 300, 1024, 4096, 10000):
+                m = lib.SequenceMixer(B, N, H, Hkv, D, dtype, lg, freq, w, w, training=training)
+                need = [lib.solar_decay_workspace_bytes(B, N, H, Hkv, D, code, False)]
+                if training:
+                    need += [lib.solar_decay_workspace_bytes(B, N, H, Hkv, D, code, True), lib.solar_layer_norm_workspace_bytes(B * N, H, D)]
+                assert m.workspace.numel() >= max(need), (B, N, H, Hkv, D)
+
+
+def decay(lib, **k):
+    a = dict(Q=P[0], K=P[1], V=P[2], log_decay=P[3], lengths=None, state_in=None, B=2, N=1024, H=4, Hkv=2, D=64, scale=1.0, t=1,
+             strides=None, O=P[4], state_out=None, workspace=P[5], bytes=1 << 40, stream=None)
+    a.update(k)
+    return lib._lib.solar_decay_attention(*a.values())
+
+
+def decay_bw(lib, **k):
+    a = dict(Q=P[0], K=P[1], V=P[2], dO=P[3], log_decay=P[4], lengths=None, state_in=None, dstate_out=None, B=2, N=1024, H=4, Hkv=2,
+             D=64, scale=1.0, t=1, strides=None, dQ=P[5], dK=P[6], dV=P[7], dstate_in=None, dlog_decay=None, workspace=P[8],
+             bytes=1 << 50, stream=None)
+    a.update(k)
+    return lib._lib.solar_decay_attention_backward(*a.values())
+
+
+def test_forward_workspace(lib):
+    need = lib.solar_decay_workspace_bytes(2, 1024, 4, 2, 64, 1, False)
+    assert need > 0
+    for k in ({"workspace": None}, {"workspace": P[5] + 16}, {"bytes": need - 1}, {"bytes": 0}):
+        assert decay(lib, **k) == WORKSPACE, k
+        assert decay(lib, O=None, Q=None, state_out=P[6], **k) == WORKSPACE, k
