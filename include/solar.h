@@ -398,7 +398,8 @@ solar_status solar_decay_attention_backward(const void* Q, const void* K, const 
 /*
  * Layer norm of every group of d columns: y = (x - mean) rstd weight + bias, rstd = 1/sqrt(mean((x - mean)^2) + eps).
  * groups = 1 is the norm of whole rows; groups = H, d = D the norm of every head of [rows, H D], which a linear attention
- * without a normalizer is followed by.
+ * without a normalizer is followed by.  Rows are contiguous and all of them count: there are no lengths here, so a padded row of
+ * zeros comes out as the bias, and in the gradient its dOut counts like any other's.
  *   In      in [rows, groups, d] of type t_in         weight, bias  in [groups, d] float, each may be NULL (1, 0)
  *   Out     out [rows, groups, d] of type t_out; may be In itself if the two types are the same
  *   mean, rstd  out [rows, groups] float, for the gradient; each may be NULL

@@ -547,7 +547,8 @@ class DeviceBatch:
 class SequenceMixer:
     """A mixing layer over sequences in their order, from the sequence operators: rotary positions on queries and keys, linear
     attention with a decay for each head, layer norm of every head's output.  Holds the buffers of one batch of B users with up
-    to N rows, the states that single tokens go on from, and with `training` the gradients.
+    to N rows, the states that single tokens go on from, and with `training` the gradients.  Rows at or past a length hold anything
+    in the inputs and come out zero.  Whole sequences start from states of zeros at position 0.
 
     log_decay [H] float, freq [rot/2] double, weight and bias [H,D] float: device tensors."""
 
@@ -587,8 +588,14 @@ class SequenceMixer:
         if lengths is None:
             self.positions.fill_(self.N)
         else:
+            self.Y.masked_fill_(self._past(), 0.0)
             self.positions.copy_(lengths[:, None])
         return self.Y
+
+    def _past(self):
+        """[B,N,1,1] truth values of the rows at or past the last forward call's lengths.  The norm knows none: a row of zeros gets
+        its bias, and adds its gradient to the bias's."""
+        return (torch.arange(self.N, device=self._lengths.device) >= self._lengths[:, None])[:, :, None, None]
 
     def step(self, Q, K, V):
         """Y [B,1,H,D] for the next token of every user: Q [B,1,H,D], K and V [B,1,Hkv,D], K and Q rotated in place."""
@@ -600,7 +607,10 @@ class SequenceMixer:
         return Y
 
     def backward(self, dY):
-        """Gradients of the last forward call: (dQ, dK, dV); dweight, dbias and dlog_decay are left in attributes."""
+        """Gradients of the last forward call: (dQ, dK, dV); dweight, dbias and dlog_decay are left in attributes.  What dY holds in
+        rows at or past the lengths does not matter."""
+        if self._lengths is not None:
+            dY = dY.masked_fill(self._past(), 0.0)
         solar_layer_norm_backward(self.O, self.weight, self.mean, self.rstd, dY, self.dO, self.dweight, self.dbias,
                                   self.workspace)
         solar_decay_attention_backward(self.Q, self.K, self._V, self.dO, self.log_decay, self._lengths, self.scale, None, None,

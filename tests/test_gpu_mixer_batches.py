@@ -1,5 +1,5 @@
 """The mixing layer on the batches of training and serving: sizes at which the forward pass is cut into parts and the gradients are
-not.  Bounds as in test_gpu_mixer.py, errors in the 2-norm."""
+not, padded rows that hold anything.  Bounds as in test_gpu_mixer.py, errors in the 2-norm."""
 import pytest
 import torch
 
@@ -37,3 +37,31 @@ def test_training_with_as_many_states_as_workgroups(lib, B, N, H, D):
         assert off(y[i:i + 1], z.double().cpu()) < 2.4e-2
         for a, e in zip(grads, one.backward(dy[i:i + 1])):
             assert off(a[i:i + 1], e.double().cpu()) < 4e-2
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("dy_dtype", [torch.bfloat16, torch.float32])
+def test_padding_holds_anything(lib, dtype, dy_dtype):
+    """Rows past the length come out zero, and what dY holds there reaches no gradient: equal bit for bit to those of a dY of zeros."""
+    B, N, H, Hkv, D = 4, 70, 4, 2, 64
+    g = torch.Generator().manual_seed(5)
+    lg, w, b = (x.cuda() for x in parameters(H, D, g))
+    freq = lib.solar_rotary_frequencies(D).cuda()
+    q, k, v = (torch.randn(B, N, h, D, generator=g).to(dtype) for h in (H, Hkv, Hkv))
+    dy = torch.randn(B, N, H, D, generator=g).to(dy_dtype)
+    n = torch.tensor([N, 0, 33, 64], dtype=torch.int32)
+    past = torch.arange(N)[None, :] >= n[:, None]
+    m = lib.SequenceMixer(B, N, H, Hkv, D, dtype, lg, freq, w, b, training=True)
+    results = []
+    for value in (0.0, 1.0, float("nan"), float("inf")):
+        for x in (q, k, v, dy):
+            x[past] = value
+        given = dy.cuda()
+        y = m.forward(q.cuda(), k.cuda(), v.cuda(), n.cuda())
+        assert (y.cpu()[past] == 0).all()
+        grads = m.backward(given)
+        assert torch.equal(given.cpu().nan_to_num(7.0), dy.nan_to_num(7.0))       # the caller's tensor is as it was
+        results.append([x.clone() for x in (y, *grads, m.dweight, m.dbias, m.dlog_decay)])
+    for r in results[1:]:
+        assert all(torch.equal(x, e) for x, e in zip(r, results[0]))
+    assert (m.dbias.double().cpu() - dy.double()[~past].sum(0)).abs().max() <= (B * N + 1) * 2.0 ** -24 * dy.double()[~past].abs().sum(0).max()
