@@ -589,7 +589,7 @@ class SequenceMixer:
             self.positions.fill_(self.N)
         else:
             self.Y.masked_fill_(self._past(), 0.0)
-            self.positions.copy_(lengths[:, None])
+            self.positions.copy_(lengths.clamp(0, self.N)[:, None])     # as the operators take them
         return self.Y
 
     def _past(self):

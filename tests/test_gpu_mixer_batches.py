@@ -1,8 +1,9 @@
 """The mixing layer on the batches of training and serving: sizes at which the forward pass is cut into parts and the gradients are
-not, padded rows that hold anything.  Bounds as in test_gpu_mixer.py, errors in the 2-norm."""
+not, padded rows that hold anything, lengths out of range.  Bounds as in test_gpu_mixer.py, errors in the 2-norm."""
 import pytest
 import torch
 
+import plain_sequence as plain
 from test_gpu_mixer import off
 
 pytestmark = pytest.mark.gpu
@@ -65,3 +66,29 @@ def test_padding_holds_anything(lib, dtype, dy_dtype):
     for r in results[1:]:
         assert all(torch.equal(x, e) for x, e in zip(r, results[0]))
     assert (m.dbias.double().cpu() - dy.double()[~past].sum(0)).abs().max() <= (B * N + 1) * 2.0 ** -24 * dy.double()[~past].abs().sum(0).max()
+
+
+@pytest.mark.parametrize("dtype,bound", [(torch.float32, 2e-5), (torch.bfloat16, 1.2e-2)])
+def test_steps_after_lengths_out_of_range(lib, dtype, bound):
+    """A length outside [0, N] is the nearer end, for the state and for the positions that steps go on from."""
+    B, N, H, Hkv, D = 3, 40, 2, 1, 64
+    g = torch.Generator().manual_seed(6)
+    lg, w, b = parameters(H, D, g)
+    freq = lib.solar_rotary_frequencies(D)
+    q, k, v = (torch.randn(B, N + 3, h, D, generator=g).to(dtype) for h in (H, Hkv, Hkv))
+    m = lib.SequenceMixer(B, N, H, Hkv, D, dtype, lg.cuda(), freq.cuda(), w.cuda(), b.cuda())
+    n = torch.tensor([-7, N + 1000, 11], dtype=torch.int32)
+    m.forward(*(x[:, :N].contiguous().cuda() for x in (q, k, v)), n.cuda())
+    n = n.clamp(0, N)
+    assert m.positions.cpu()[:, 0].tolist() == n.tolist()
+    users = torch.arange(B)
+    for i in range(3):
+        at = (n + i).long()
+        y = m.step(*(x[users, at][:, None].contiguous().cuda() for x in (q, k, v)))
+        for u in range(B):
+            rows = [x[u:u + 1, :at[u] + 1].double() for x in (q, k, v)]
+            pos = torch.arange(int(at[u]) + 1)[None, :]
+            o, _ = plain.decay_attention(plain.rotary(rows[0], pos, freq), plain.rotary(rows[1], pos, freq), rows[2], lg.double(), None, None,
+                                         D ** -0.5)
+            want = plain.layer_norm(o[0], w.double(), b.double(), 1e-5)[0][-1]
+            assert off(y[u, 0], want) < bound, (i, u)
