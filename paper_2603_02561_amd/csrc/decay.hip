@@ -28,8 +28,7 @@ __global__ __launch_bounds__(kThreads) void decay_rows_kernel(Walk w) {
     const int slice = blockIdx.x % NS, h = blockIdx.x / NS % w.H, b = blockIdx.x / NS / w.H;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int row0 = (tid >> 3) * RPT, col = slice * kSlice + 4 * (tid & 7);
-    // g - 1, and g x as x + (g - 1) x: over thousands of rows the error of a rounded g would add up, near g = 1 in particular
-    const float g1 = expm1f(w.log_decay[h]);
+    const Kept g = kept(w.log_decay[h], 1);
     const size_t at = ((size_t)b * w.H + h) * D * D;
     const int len = user_len(w.lengths, b, w.N);
     float S[RPT][4];
@@ -51,7 +50,7 @@ __global__ __launch_bounds__(kThreads) void decay_rows_kernel(Walk w) {
             const float kr = load1<BF16>(k, row0 + r), qr = load1<BF16>(q, row0 + r);
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
-                S[r][c] = fmaf(kr, vv[c], fmaf(S[r][c], g1, S[r][c]));
+                S[r][c] = fmaf(kr, vv[c], keep(S[r][c], g));
                 o[c] = fmaf(qr, S[r][c], o[c]);
             }
         }

@@ -8,8 +8,8 @@
 // read; only P = Q K^T o M goes through LDS, each wave forming a share of it.
 //
 // Precision.  Sums and S are float.  The matrix unit takes bf16, so a float operand is cut into bf16 terms that add up to it:
-// three, which hold all 24 bits.  Products of two such operands (float inputs) take the six pairs of terms above 2^-24.  g^C S is
-// S + (g^C - 1) S, so that the error of a rounded g^C does not add up over the chunks.
+// three, which hold all 24 bits.  Products of two such operands (float inputs) take the six pairs of terms above 2^-24.  The error
+// of a rounded g^C does not add up over the chunks, nor is a small one lost (Kept, sequence.h).
 //
 // What bounds it: not memory (64 users of 10000 rows at D = 128: 655 MB, 130 us at the rate of a copy; 190 us, of which the kernel
 // without its loads and stores takes 155) but the instructions of a chunk: per wave 204 matrix instructions, 3300 cycles, and 800 of
@@ -347,7 +347,20 @@ decay_chunk_kernel(Walks ws) {
         v_at = NB == 2 ? trow * W + (((4 * wave + (c16 & 3)) ^ swizzle<W>(trow)) << 3)
                        : trow * W + (((2 * wave + (c16 >> 1 & 1)) ^ swizzle<W>(trow)) << 3) + 4 * (c16 & 1);
     }
-    const float gfull = expm1f(lg * (float)C);
+    // A chunk keeps (hi + lo) S: S is multiplied by a float, which also makes good what the ones before have rounded away (`owed`,
+    // relative to S; one instruction an entry)
+    struct Factor {
+        float hi, lo;
+    };
+    auto uniform = [](float x) { return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(x))); };
+    auto factor = [&](int n) {
+        const Kept k = kept(lg, n);
+        const float hi = k.near ? 1.f + k.by : k.by, y = hi - 1.f;
+        return Factor{uniform(hi), uniform(k.near ? (1.f - (hi - y)) + (k.by - y) : 0.f)};
+    };
+    const Factor full = factor(C), last = factor(count % C);
+    const float inverse = uniform(full.hi < 0.5f ? 0.f : 1.f / full.hi);
+    float owed = 0.f;
     double z = 0.;          // terms of either sign over thousands of rows
 
     for (int done = 0; done < count; done += C) {
@@ -623,7 +636,9 @@ decay_chunk_kernel(Walks ws) {
         if constexpr (OUT) fq.load(qr, done + C, count);
 
         // S <- g^cnt S + K^T diag(g^(cnt-pre-j)) V, and T <- g^cnt (T + cnt S) + ... with the weights' derivative
-        const float gc = cnt == C ? gfull : expm1f(lg * (float)cnt);
+        const Factor k = cnt == C ? full : last;
+        const float fix = fmaf(owed, k.hi, k.lo), g = uniform(k.hi + fix);
+        owed = uniform((fix - (g - k.hi)) * inverse);
 #pragma unroll
         for (int j = 0; j < NJ; ++j)
 #pragma unroll
@@ -632,12 +647,10 @@ decay_chunk_kernel(Walks ws) {
                 for (int a = 0; a < 2; ++a)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        if constexpr (MOMENT) {
-                            const float x = fmaf((float)cnt, S[j][nb][a][i], T[j][nb][a][i]);
-                            T[j][nb][a][i] = fmaf(x, gc, x);
-                        }
-                        S[j][nb][a][i] = fmaf(S[j][nb][a][i], gc, S[j][nb][a][i]);
+                        if constexpr (MOMENT) T[j][nb][a][i] = fmaf((float)cnt, S[j][nb][a][i], T[j][nb][a][i]) * g;
+                        S[j][nb][a][i] *= g;
                     }
+        if constexpr (MODE != kMoment) __builtin_amdgcn_sched_barrier(0);       // or registers are spilled
 #pragma unroll
         for (int kk = 0; kk < NK; ++kk) {
             v8bf kt[2][2][NT];
@@ -724,19 +737,20 @@ __global__ __launch_bounds__(kJoinThreads) void join_parts_kernel(Walk w) {
     const int all = w.nparts * w.pieces, last = all - w.pieces, piece_rows = w.part_rows / w.pieces;
     float* p = w.parts + bh * all * DD + e;
     float* pm = MOMENT ? w.part_moments + bh * all * DD + e : nullptr;
+    const Kept whole = kept(lg, piece_rows);
     for (int o = 0; o < last; ++o) {
         const int part = w.reverse ? all - 1 - o : o, row0 = part * piece_rows;
         const int rows = w.N - row0 < piece_rows ? w.N - row0 : piece_rows;
         const int count = len - row0 < 0 ? 0 : (len - row0 < rows ? len - row0 : rows);
-        const float g = expm1f(lg * (float)count), gc = count ? g : 0.f;      // log g may be -infinity
+        const Kept g = count == piece_rows ? whole : kept(lg, count);
         if constexpr (MOMENT) {
             const float add = pm[(size_t)o * DD], x = fmaf((float)count, s, t);
             if (o % w.pieces == 0) pm[(size_t)o * DD] = t;
-            t = fmaf(x, gc, x) + add;
+            t = (count ? keep(x, g) : t) + add;
         }
         const float add = p[(size_t)o * DD];
         if (o % w.pieces == 0) p[(size_t)o * DD] = s;
-        s = fmaf(s, gc, s) + add;
+        s = (count ? keep(s, g) : s) + add;
     }
     p[(size_t)last * DD] = s;
     if constexpr (MOMENT) pm[(size_t)last * DD] = t;

@@ -22,6 +22,18 @@ __device__ __forceinline__ char* row_of(const Heads& t, int b, int64_t n, int h)
     return t.data + b * t.s.batch + n * t.s.row + (int64_t)(h / t.share) * t.s.head;
 }
 
+// What a state keeps over n rows, g^n x.  Near 1 that is x + (g^n - 1) x, or the error of a rounded g^n would add up over thousands of
+// steps; below a half g^n - 1 has lost bits that count, and it is g^n x: what is left of a large first state may be all there is.
+struct Kept {
+    float by;
+    bool near;      // by is g^n - 1, else g^n
+};
+__device__ __forceinline__ Kept kept(float log_g, int n) {
+    const float x = log_g * (float)n, m = expm1f(x);
+    return {m < -0.5f ? expf(x) : m, !(m < -0.5f)};
+}
+__device__ __forceinline__ float keep(float x, Kept k) { return fmaf(x, k.by, k.near ? x : 0.f); }
+
 // One walk over the rows of every user and head with a state S [D,D]:
 //   forward   S = g S + k_t v_t^T,  o_t = o_scale S^T q_t          rows 0 .. len - 1
 //   reverse   S += k_t v_t^T,  o_t = o_scale S^T q_t,  S = g S     rows len - 1 .. 0
