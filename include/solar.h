@@ -366,7 +366,7 @@ solar_status solar_rotary(const void* Q, const void* K, const int32_t* lengths, 
  *              length 0 keeps its state
  * Sums and states are float.  A NaN or an infinity in a valid row changes outputs of its own row and later ones only (an
  * infinity may come out as NaN).  O overlaps no input.
- * Supported: D in {64, 128, 256}, N <= 2^30, rows less than 16 MB apart.  Workspace: solar_decay_workspace_bytes(B, N, H, Hkv, D,
+ * Supported: D in {64, 128, 256}, N <= 2^30, B H D < 2^27, rows less than 16 MB apart.  Workspace: solar_decay_workspace_bytes(B, N, H, Hkv, D,
  * t, 0) bytes, which may be 0, 256-byte aligned.
  */
 size_t solar_decay_workspace_bytes(int B, int N, int H, int Hkv, int D, solar_dtype t, int backward);
@@ -385,7 +385,8 @@ solar_status solar_decay_attention(const void* Q, const void* K, const void* V, 
  *   strides     in HOST memory [7]: Q, K, V, dO, dQ, dK, dV; NULL: all contiguous
  *   dQ, dK, dV  out, of type t, rows at or past the valid length zero
  *   dstate_in   out [B,H,D,D] float or NULL       dlog_decay  out [H] float or NULL
- * Outputs overlap nothing.  Workspace: solar_decay_workspace_bytes(B, N, H, Hkv, D, t, 1), 256-byte aligned.  It may be less
+ * Outputs overlap nothing.  Supported: as above, and where heads share K and V also H D <= 2^22 and B N Hkv D <= 2^34 - 1024.
+ * Workspace: solar_decay_workspace_bytes(B, N, H, Hkv, D, t, 1), 256-byte aligned.  It may be less
  * than the operator's own: a buffer for both takes the larger of the two.
  */
 solar_status solar_decay_attention_backward(const void* Q, const void* K, const void* V, const void* dO,

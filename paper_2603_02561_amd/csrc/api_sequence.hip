@@ -58,8 +58,10 @@ solar_status check_decay(int B, int N, int H, int Hkv, int D, float scale, solar
         return SOLAR_ERR_INVALID_ARG;
     if (D != 64 && D != 128 && D != 256) return SOLAR_ERR_UNSUPPORTED;
     if (N > 1 << 30) return SOLAR_ERR_UNSUPPORTED;
-    // Workgroups of the row form go by users, heads and slices; those of the chunked form are fewer, but twice the size and for two
-    // walks at once, and parts are only cut where there are less than 512.
+    // Workgroups of the row form go by users, heads and slices of 32 columns.  Those of the chunked form go by users and shared heads,
+    // rounded up to a multiple of eight, times the heads that share one: B = 1 with one K head makes eight times H, at slices of at least
+    // twice the columns and up to 512 threads: less than 2^32 threads too, the most that a launch takes.  Parts are only cut where
+    // there are less than 512; the gradients' two walks run at once, but with shared heads H D <= 2^22.
     if ((int64_t)B * H * (D / 32) > kMaxBlocks / 4) return SOLAR_ERR_UNSUPPORTED;
     return SOLAR_OK;
 }
@@ -238,10 +240,10 @@ solar_status solar_decay_attention_backward(const void* Q, const void* K, const 
         return SOLAR_ERR_INVALID_ARG;
     for (const Heads& x : {q, k, vv, g, dq, dk, dv})
         if (!rows_near(x)) return SOLAR_ERR_UNSUPPORTED;
-    if ((int64_t)H * D > 1 << 22) return SOLAR_ERR_UNSUPPORTED;      // rows of the float work arrays
+    // rows of the float work arrays, and a thread for every four columns of their sums
+    if (share > 1 && ((int64_t)H * D > 1 << 22 || (int64_t)B * N * Hkv * (D / 4) > kMaxBlocks * 256)) return SOLAR_ERR_UNSUPPORTED;
     const DecayCarve c = carve_decay(workspace, B, N, H, Hkv, D, true);
     if (c.total && (!workspace || workspace_bytes < c.total || misaligned(workspace, 256))) return SOLAR_ERR_WORKSPACE;
-    if ((int64_t)B * N * Hkv * (D / 4) > kMaxBlocks * 256) return SOLAR_ERR_UNSUPPORTED;
     hipStream_t st = (hipStream_t)stream;
     Walk w = {};
     w.lengths = lengths;

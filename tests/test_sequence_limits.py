@@ -55,3 +55,31 @@ def test_forward_workspace(lib):
     for k in ({"workspace": None}, {"workspace": P[5] + 16}, {"bytes": need - 1}, {"bytes": 0}):
         assert decay(lib, **k) == WORKSPACE, k
         assert decay(lib, O=None, Q=None, state_out=P[6], **k) == WORKSPACE, k
+
+
+def by_heads(N, *heads):
+    """[B,heads,N,64] for B = 1: rows next to each other, heads N rows apart."""
+    return strides(*(x for h in heads for x in (0, 64, 64 * N)))
+
+
+def test_launches_of_too_many_workgroups_are_refused(lib):
+    """2^22 slices of 32 columns are too many, however the heads share K and V."""
+    N = 16
+    for D, H in ((64, 1 << 21), (128, 1 << 20), (256, 1 << 19)):
+        for Hkv in (1, H):
+            s = strides(*([0, D, D * N] * 4))
+            assert decay(lib, B=1, N=N, H=H, Hkv=Hkv, D=D, strides=s) == UNSUPPORTED, (D, H)
+            assert decay(lib, B=1, N=1, H=H, Hkv=Hkv, D=D, strides=s) == UNSUPPORTED, (D, H)
+
+
+def test_limits_of_the_gradients(lib):
+    """Float gradients of every head are added where K and V are shared, and only there: [B,N,H,D] of them has rows of less than 16 MB
+    and no more vectors than a launch has threads.  Nothing runs here: a call that passes the checks stops at the workspace."""
+    N, few = 16, {"workspace": None}
+    s = by_heads(N, *range(7))
+    assert decay_bw(lib, B=1, N=N, H=1 << 17, Hkv=1 << 17, strides=s, **few) == WORKSPACE
+    assert decay_bw(lib, B=1, N=N, H=1 << 17, Hkv=1 << 16, strides=s, **few) == UNSUPPORTED
+    assert decay_bw(lib, B=1, N=N, H=1 << 15, Hkv=1 << 14, strides=s, **few) == WORKSPACE
+    # 2^32 vectors of four columns
+    assert decay_bw(lib, B=1 << 8, N=1 << 17, H=8, Hkv=8, **few) == WORKSPACE
+    assert decay_bw(lib, B=1 << 8, N=1 << 17, H=16, Hkv=8, **few) == UNSUPPORTED
