@@ -345,7 +345,7 @@ solar_status solar_rotary_frequencies(int rot, double base, solar_rotary_scaling
  *   inverse    nonzero: -x instead of x.  With the same amplitude this is the gradient: dQ from dQout
  *   strides    in HOST memory [4]: Q, K, Qout, Kout; NULL: all contiguous
  *   Qout, Kout  out; each may be its input, with the same strides.  Rows at or past the valid length come out zero
- * Supported: D a multiple of 8 up to 512, rot even, 2 <= rot <= D, B * N < 2^24.
+ * Supported: D a multiple of 8 up to 512, rot even, 2 <= rot <= D, B * N <= 2^26 - 4, up to 65536 heads of Q and K together.
  */
 solar_status solar_rotary(const void* Q, const void* K, const int32_t* lengths, const int32_t* positions,
                           const double* freq, int B, int N, int H, int Hkv, int D, int rot, solar_rotary_layout layout,

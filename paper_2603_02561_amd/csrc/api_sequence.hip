@@ -153,7 +153,7 @@ solar_status solar_rotary(const void* Q, const void* K, const int32_t* lengths, 
                                               r.in[i].s.head != r.out[i].s.head))
             return SOLAR_ERR_INVALID_ARG;
     if (K && (Qout == K || Kout == Q || Qout == Kout)) return SOLAR_ERR_INVALID_ARG;
-    if ((int64_t)B * N > kMaxBlocks || (int64_t)H + (K ? Hkv : 0) > 65536) return SOLAR_ERR_UNSUPPORTED;
+    if ((int64_t)B * N > kMaxBlocks * kRotaryRows || (int64_t)H + (K ? Hkv : 0) > 65536) return SOLAR_ERR_UNSUPPORTED;
     r.heads[0] = H;
     r.heads[1] = K ? Hkv : 0;
     r.lengths = lengths;

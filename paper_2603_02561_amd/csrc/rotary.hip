@@ -175,8 +175,7 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(Rotary r, int tokens, 
 
 hipError_t launch_rotary(const Rotary& r, hipStream_t stream) {
     const int pairs = r.rot / 2;
-    // four rows a workgroup: 256 angles at 128 rotated columns, one a thread
-    const int tokens = 4;
+    const int tokens = kRotaryRows;
     const int64_t all = (int64_t)r.B * r.N;
     const dim3 grid((unsigned)((all + tokens - 1) / tokens)), block(kThreads);
     const size_t lds = sizeof(float2) * tokens * pairs;

@@ -99,6 +99,7 @@ struct Rotary {
     bool interleaved, inverse, bf16;
     float amplitude;
 };
+constexpr int kRotaryRows = 4;      // of a workgroup: 256 angles at 128 rotated columns, one a thread
 hipError_t launch_rotary(const Rotary& r, hipStream_t stream);
 
 // norm.hip

@@ -83,3 +83,14 @@ def test_limits_of_the_gradients(lib):
     # 2^32 vectors of four columns
     assert decay_bw(lib, B=1 << 8, N=1 << 17, H=8, Hkv=8, **few) == WORKSPACE
     assert decay_bw(lib, B=1 << 8, N=1 << 17, H=16, Hkv=8, **few) == UNSUPPORTED
+
+
+def test_rotary_rows(lib):
+    """A workgroup takes four rows: 2^24 - 1 of them are the most."""
+    def rotary(B, N):
+        return lib._lib.solar_rotary(P[0], None, None, None, P[1], B, N, 1, 1, 8, 8, 0, 0, 1.0, 0, None, P[0], None, None)
+
+    most = 4 * ((1 << 24) - 1)
+    assert rotary(1, most + 1) == UNSUPPORTED and rotary(4, 1 << 24) == UNSUPPORTED
+    if not torch.cuda.is_available():           # only where no launch can follow
+        assert rotary(1, most) not in (UNSUPPORTED, INVALID) and rotary(1, 1 << 24) not in (UNSUPPORTED, INVALID)
