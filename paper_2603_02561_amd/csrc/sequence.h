@@ -70,10 +70,10 @@ struct Walks {
 
 // decay.hip
 // A forward walk row by row, for a few rows (N <= kDecayRows); nparts is not looked at.  Every row costs it a sum across the
-// workgroup, the chunked form takes up to 32 or 64 rows at the price of one: 4 rows of 1024 states take 15.3 against 16.2 us at
-// D = 64, 32.5 against 37.4 at 128, 8 rows 22.2 against 16.1 and 44.5 against 37.4 (bf16; four states 5.6 against 6.6 and 8.7
-// against 6.6 at D = 64).
-constexpr int kDecayRows = 4;
+// workgroup, the chunked form takes up to 32 or 64 rows at the price of one.  Six rows of 1024 states take 14.4 against 17.4 us at
+// D = 64, 36.9 against 39.2 at 128, 116 against 140 at 256, eight rows 17.5 against 17.4, 42.2 against 39.4, 130 against 141; of four states
+// 7.4 against 7.5 at D = 64 and 7.8 against 11.6 at 128, eight rows 8.9 against 7.5 and 9.5 against 11.6 (bf16).
+constexpr int kDecayRows = 6;
 hipError_t launch_decay_rows(const Walk& w, hipStream_t stream);
 // dlog[h] = the sum of moments [B][H][slices] over users and slices
 hipError_t launch_moment_sum(const double* moments, int B, int H, int slices, float* dlog, hipStream_t stream);
