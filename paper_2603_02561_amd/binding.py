@@ -548,7 +548,8 @@ class SequenceMixer:
     """A mixing layer over sequences in their order, from the sequence operators: rotary positions on queries and keys, linear
     attention with a decay for each head, layer norm of every head's output.  Holds the buffers of one batch of B users with up
     to N rows, the states that single tokens go on from, and with `training` the gradients.  Rows at or past a length hold anything
-    in the inputs and come out zero.  Whole sequences start from states of zeros at position 0.
+    in the inputs and come out zero.  Whole sequences start from states of zeros at position 0; rotations
+    have amplitude 1.
 
     log_decay [H] float, freq [rot/2] double, weight and bias [H,D] float: device tensors."""
 

@@ -3,8 +3,8 @@
 //
 // The state is cut into slices of 32 columns, one workgroup each: eight lanes hold four columns, 32 groups of lanes hold
 // D / 32 rows each, in registers from the first row of the sequence to the last.  A row costs one sum over the groups
-// (three steps across lanes, one through LDS).  2048 states of 128 x 128 a step: 268 MB read and written in 51 us, launch and
-// all (5.3 TB/s; a large copy 5.1).
+// (three steps across lanes, one through LDS).  2048 states of 128 x 128 a step: 268 MB read and written in 50 us, launch and
+// all (5.4 TB/s; a large copy 5.1).
 #include "sequence.h"
 
 namespace solar {

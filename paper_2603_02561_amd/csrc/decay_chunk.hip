@@ -11,12 +11,16 @@
 // three, which hold all 24 bits.  Products of two such operands (float inputs) take the six pairs of terms above 2^-24.  The error
 // of a rounded g^C does not add up over the chunks, nor is a small one lost (Kept, sequence.h).
 //
-// What bounds it: not memory (64 users of 10000 rows at D = 128: 655 MB, 130 us at the rate of a copy; 190 us, of which the kernel
-// without its loads and stores takes 155) but the instructions of a chunk: per wave 204 matrix instructions, 3300 cycles, and 800 of
-// the vector ALU, most of them the terms of S, P and the weighted V; the two overlap only in part.  A workgroup per compute unit takes
-// nearly as long as two do for twice the work (179 us against 155 without memory).  Tried without gain: sixteen columns per wave
-// with twice the waves (twice the reads of Q and K from LDS: 186 us against 188), loads issued earlier in the chunk, vector
-// instructions between the matrix instructions by schedule groups (+3 %).
+// What bounds it: not memory (64 users of 10000 rows at D = 128: 655 MB, 130 us at the rate of a copy; 226 to 235 us) but the
+// instructions of a chunk and the waits between them.  Per wave and chunk there are 240 matrix instructions, 3840 cycles, and 1020 of the
+// vector ALU, 4070, most of them the terms of S, P and the weighted V.  By the counters the matrix unit is busy 34 % of the time and the
+// vector ALU 36 %, both at once only 6 %; LDS 32 %.  A wave spends 23 % of its time waiting for LDS, memory or the others: there are
+// three barriers a chunk, between which the waves of a workgroup run the same phase, and two waves to a SIMD.  With log g's derivative
+// there is one workgroup to a compute unit: matrix unit 27 %, vector ALU 32 %, both 5 %, and 53 % of a wave's time is waiting.
+// In that form registers are spilled: 37 at D = 128 and 274 at 256, 63 and 540 for float rows; the others spill a few at D = 256 with
+// float rows, and outside the usual path at 128.  S and P in two terms (16 bits) took 8 to 10 % less.  Tried without gain, with those: sixteen
+// columns per wave with twice the waves (twice the reads of Q and K from LDS: 186 us against 188), loads issued earlier in the
+// chunk, vector instructions between the matrix instructions by schedule groups (+3 %).
 #include "kernels.h"
 #include "sequence.h"
 
@@ -131,7 +135,8 @@ __device__ __forceinline__ void products(const v8bf (&a)[M][TA], const v8bf (&b)
 
 // The images of rows in LDS have no padding: chunks of eight elements lie in row `row` at the place (chunk ^ swizzle(row)).  Then
 // neither the reads of one chunk from sixteen rows, nor the transposing reads of four rows, nor the stores of whole rows meet
-// in a bank (a row is 32, 64 or 128 of the 64 banks long).
+// in a bank (a row is 32, 64 or 128 of the 64 banks long).  The counters put 41 % of the busy time of LDS down to conflicts all the same,
+// of accesses that they do not name.
 template <int COLS>
 __device__ __forceinline__ int swizzle(int row) {
     if constexpr (COLS == 64) return ((row >> 1 & 1) << 2) | (row >> 2 & 3);
