@@ -92,3 +92,36 @@ def test_steps_after_lengths_out_of_range(lib, dtype, bound):
                                          D ** -0.5)
             want = plain.layer_norm(o[0], w.double(), b.double(), 1e-5)[0][-1]
             assert off(y[u, 0], want) < bound, (i, u)
+
+
+def test_captured_with_lengths(lib):
+    """A ragged training step captured once and replayed with other inputs and lengths, between eager calls of the same layer."""
+    B, N, H, Hkv, D = 3, 300, 4, 2, 64
+    g = torch.Generator().manual_seed(8)
+    lg, w, b = (x.cuda() for x in parameters(H, D, g))
+    freq = lib.solar_rotary_frequencies(D).cuda()
+    q, k, v, dy = (torch.randn(B, N, h, D, generator=g).bfloat16().cuda() for h in (H, Hkv, Hkv, H))
+    n = torch.tensor([N, 17, 0], dtype=torch.int32, device="cuda")
+    m = lib.SequenceMixer(B, N, H, Hkv, D, torch.bfloat16, lg, freq, w, b, training=True)
+
+    def both():
+        return (m.forward(q, k, v, n), *m.backward(dy), m.dweight, m.dbias, m.dlog_decay, m.state, m.positions)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        both()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        outs = both()
+    for i in range(3):
+        q.copy_(torch.randn(q.shape, generator=torch.Generator().manual_seed(i)))
+        n.copy_(torch.tensor([N - 50 * i, 17 + i, N if i else 0], dtype=torch.int32))
+        want = [x.clone() for x in both()]
+        for x in outs:
+            x.fill_(7)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(outs, want)), i
